@@ -30,7 +30,8 @@
  *     per-step calls (everything but gs_create, gs_destroy, gs_step_profiled and
  *     gs_timing_*) neither allocate, synchronize nor clear memory with a memset, so they
  *     can be captured in a HIP graph and replayed.
- *   - Inputs must be finite; results for NaN or infinite inputs are unspecified.
+ *   - Inputs must be finite; results for NaN or infinite inputs are unspecified (the
+ *     language-model operators at the end say what they do with them).
  */
 #ifndef GS_H
 #define GS_H
@@ -291,12 +292,148 @@ typedef struct gs_plan {
 } gs_plan;
 gs_status gs_describe(const gs_ctx* ctx, gs_plan* out);
 
+/* ---------------------------------------------------------------------------------------
+ * Operators of a recurrent language model: what a training step of one computes between its
+ * matrix products, and whose weight gradients the calls above then compress (the paper's
+ * LSTM language model is the workload of that size). They need no context.
+ *
+ *   - Activations are GS_F32, GS_BF16 or GS_F16, one type per call; sums, states, losses and
+ *     statistics are fp32, and a result is rounded to the activations' type once, on its store.
+ *   - Sizes may be zero (nothing is computed and array arguments may be NULL). Offsets are
+ *     64-bit throughout.
+ *   - Arrays must be aligned to their elements. Wider alignment and even sizes only make the
+ *     calls faster.
+ *   - Calls are independent of each other: they share no memory but their arguments, neither
+ *     allocate nor synchronize, and can be captured in a HIP graph. Results are the same bits
+ *     on every run.
+ *   - Messages of failing calls: gs_last_error(NULL).
+ */
+#define GS_F32 0
+#define GS_BF16 1
+#define GS_F16 2
+
+/* A [B][T][C] array: element (b, t, c) is data[b*batch + t*time + c] (strides in elements, not
+ * negative; inputs may overlap each other, as slices of one projection do). */
+typedef struct gs_rows {
+  void* data;
+  int64_t batch;
+  int64_t time;
+} gs_rows;
+
+/* Gated linear recurrence over T steps of B sequences of C channels. With a = sigmoid(f):
+ *     h_t = a_t h_(t-1) + (1 - a_t) x_t,     y_t = sigmoid(o_t) h_t   (y_t = h_t without o)
+ * from h_0. Positions t >= lengths[b] are padding: x, f, o (and gy) there are not read, or
+ * read and not used, whatever they hold; the state passes them unchanged and y is 0.
+ *   B, T, C   sizes, each >= 0; T = 1 is the form that serves single tokens
+ *   dtype     GS_F32, GS_BF16 or GS_F16: the type of x, f, o, y and their gradients
+ *   x, f, o   [B][T][C] inputs: candidates, forget-gate and output-gate pre-activations;
+ *             o.data NULL: no output gate
+ *   lengths   [B] int32 or NULL (all T); values outside [0, T] are taken as the nearer end
+ *   h0        [B][C] fp32 or NULL (zero)
+ * Errors: GS_ERR_INVALID_ARG (nothing is enqueued) for sizes or strides below zero, an unknown
+ * dtype, a NULL array, an array not aligned to its elements; GS_ERR_UNSUPPORTED for B, T or C
+ * over 2^31 - 1 or, with T > 1, a time stride over GS_RECURRENCE_MAX_STRIDE. */
+#define GS_RECURRENCE_BLOCK 128
+#define GS_RECURRENCE_BLOCKS(T) (((T) + GS_RECURRENCE_BLOCK - 1) / GS_RECURRENCE_BLOCK)
+#define GS_RECURRENCE_MAX_STRIDE 4194304
+typedef struct gs_recurrence {
+  int64_t B;
+  int64_t T;
+  int64_t C;
+  int32_t dtype;
+  gs_rows x;
+  gs_rows f;
+  gs_rows o;
+  const int32_t* lengths;
+  const float* h0;
+} gs_recurrence;
+
+/* Bytes of the `work` scratch of the two calls below at these sizes, for either direction
+ * (0: none is needed and work may be NULL; negative: sizes below zero or an unknown dtype). Its
+ * contents need not be set and are not kept for anything. */
+int64_t gs_recurrence_work(int64_t B, int64_t T, int64_t C, int32_t dtype);
+
+/* Forward. y: [B][T][C] output. h_last: [B][C] fp32 output, the state after each sequence's last
+ * token (h_0 of an empty one); it may be h0's own array. states: [B][GS_RECURRENCE_BLOCKS(T)][C]
+ * fp32 output for the backward call, the state before each block of GS_RECURRENCE_BLOCK steps
+ * that holds a token, or NULL. */
+gs_status gs_recurrence_forward(const gs_recurrence* r, void* stream, gs_rows y, float* h_last, float* states,
+                                void* work);
+
+/* Backward: with q_t = gy_t sigmoid(o_t) and s_t = q_t + a_(t+1) s_(t+1) (after the last token gh
+ * stands for a s),
+ *     dx_t = (1 - a_t) s_t,   df_t = s_t (h_(t-1) - x_t) a_t (1 - a_t),
+ *     do_t = gy_t h_t sigmoid(o_t) (1 - sigmoid(o_t)),   dh0 = a_1 s_1;   zero at padding.
+ * The states h_t are computed again from `states` of the forward call on the same inputs.
+ * gy: [B][T][C] input. gh: [B][C] fp32 input, the gradient of h_last, or NULL (zero). dx, df, dout:
+ * [B][T][C] outputs (dout.data NULL exactly when there is no o). dh0: [B][C] fp32 output or NULL.
+ * Outputs must not overlap inputs. */
+gs_status gs_recurrence_backward(const gs_recurrence* r, void* stream, gs_rows gy, const float* gh,
+                                 const float* states, gs_rows dx, gs_rows df, gs_rows dout, float* dh0, void* work);
+
+/* Dropout whose mask is drawn from a counter and never stored:
+ *     y[i] = residual[i] + (kept[i] ? x[i] * 65536 / (65536 - n) : 0),   n = floor(65536 p + 1/2)
+ * for i = row * cols + col, the product and the sum each rounded to fp32. Element i is kept when
+ * bits 16 (i mod 4) to 16 (i mod 4) + 15 of word i / 4 are not below n; word w is
+ * mix(key + (w + 1) * 0x9E3779B97F4A7C15), key = mix(mix(mix(seed) ^ step) ^ site), with mix
+ * SplitMix64's output function (Steele, Lea & Flood, OOPSLA 2014). The draws depend on nothing
+ * else, so the backward pass is the same call on the gradient, without a residual. x of dropped
+ * elements is not used, whatever it holds. p is rounded to a multiple of 1/65536, and the factor
+ * is that of the rounded p: the expectation of y is exact.
+ *   x, residual (or NULL), y: rows of `cols` contiguous elements, x_stride (res_stride, y_stride)
+ *   elements apart, at least cols; y may be x's or residual's own array.
+ *   p in [0, 1] (1: everything is dropped); seed: the program's; site: which dropout of the
+ *   program (and, with simulated workers, whose); step: DEVICE pointer to the training step, one int64,
+ *   read when the kernel runs (so a captured graph draws a new mask on each replay), or NULL (0). */
+gs_status gs_dropout(void* stream, int32_t dtype, int64_t rows, int64_t cols, const void* x, int64_t x_stride,
+                     const void* residual, int64_t res_stride, void* y, int64_t y_stride, double p, uint64_t seed,
+                     uint64_t site, const int64_t* step);
+
+/* Softmax cross-entropy of N rows of V logits, and its gradient, in one pass over the logits:
+ *     losses[n] = log(sum_v exp(z[n][v])) - z[n][t_n],
+ *     grad[n][v] = m (softmax(z[n])[v] - [v = t_n])
+ * with m = factor * scale[n * scale_stride] (factor alone without scale), divided by the number
+ * of rows that count when `mean` is set. A row with targets[n] == ignore_index does not count: its loss
+ * and gradient are 0, whatever its logits hold. -inf logits have probability 0. A row of nothing but
+ * -inf, or with NaN or +inf, has NaN loss and gradient (the formula's); so has a row whose target is neither
+ * ignore_index nor in [0, V): it is not looked up.
+ *   logits   [N][V] input, rows logits_stride elements apart (at least V)
+ *   targets  [N] int64 input
+ *   losses   [N] fp32 output, or NULL without mean_loss
+ *   mean_loss  one fp32 output or NULL: the sum of the losses over the number of rows that count (0 when
+ *            none does)
+ *   grad     [N][V] output, rows grad_stride elements apart, or NULL; may be the logits' own array
+ *   work     scratch of gs_cross_entropy_work(N, V, dtype) bytes (negative for invalid sizes)
+ * Errors: GS_ERR_INVALID_ARG for sizes below zero, N > 0 with V = 0, strides below V, an unknown
+ * dtype, scale_stride not 0 or 1, NULL or misaligned arrays; GS_ERR_UNSUPPORTED for N or V over
+ * 2^31 - 1. */
+typedef struct gs_xent {
+  int64_t N;
+  int64_t V;
+  int32_t dtype;
+  int32_t mean;
+  const void* logits;
+  int64_t logits_stride;
+  const int64_t* targets;
+  int64_t ignore_index;
+  float factor;
+  const float* scale;
+  int64_t scale_stride;
+  float* losses;
+  float* mean_loss;
+  void* grad;
+  int64_t grad_stride;
+  void* work;
+} gs_xent;
+int64_t gs_cross_entropy_work(int64_t N, int64_t V, int32_t dtype);
+gs_status gs_cross_entropy(const gs_xent* x, void* stream);
+
 /* Static description of a status code. */
 const char* gs_status_string(gs_status status);
 
 /* Message describing the last failing call on `ctx` ("" if none); valid until the next
- * call on the context. With ctx == NULL: the last failing context-free call (gs_create or
- * gs_unsketch_topk_static) on this thread. */
+ * call on the context. With ctx == NULL: the last failing context-free call (gs_create,
+ * gs_unsketch_topk_static, the language-model operators) on this thread. */
 const char* gs_last_error(const gs_ctx* ctx);
 
 #ifdef __cplusplus

@@ -25,7 +25,8 @@ GS_MAX_ROWS = 16
 EXPORTED = ("gs_create", "gs_destroy", "gs_accumulate", "gs_sketch", "gs_merge", "gs_unsketch_topk",
             "gs_gather_reset", "gs_step", "gs_heavymix_topk", "gs_step_heavymix", "gs_step_sketch_momentum",
             "gs_apply_update", "gs_step_profiled", "gs_timing_start", "gs_timing_stop", "gs_unsketch_topk_static",
-            "gs_describe", "gs_status_string", "gs_last_error")
+            "gs_describe", "gs_recurrence_work", "gs_recurrence_forward", "gs_recurrence_backward", "gs_dropout",
+            "gs_cross_entropy_work", "gs_cross_entropy", "gs_status_string", "gs_last_error")
 GS_STATIC_MAX_D = 4194304  # largest d of gs_unsketch_topk_static (its fixed scratch array)
 GS_NUM_STAGES = 5
 STAGES = ("accumulate", "sketch", "merge", "select", "gather_reset")
@@ -37,6 +38,12 @@ STATE_LAYOUTS = {"worker_major": GS_STATE_WORKER_MAJOR, "interleaved": GS_STATE_
 def state_stride(P: int) -> int:
     """Row length of the interleaved state: P rounded up to a multiple of 4."""
     return (P + 3) // 4 * 4
+
+
+# activation types of the language-model operators, and the recurrence's block of saved states
+GS_F32, GS_BF16, GS_F16 = 0, 1, 2
+GS_RECURRENCE_BLOCK = 128
+GS_RECURRENCE_MAX_STRIDE = 4194304
 
 
 class GsLibraryMissing(RuntimeError):
@@ -77,6 +84,47 @@ class gs_plan(ctypes.Structure):
                  "row_copy")]
 
 
+class gs_rows(ctypes.Structure):
+    """A [B][T][C] array: data pointer, batch and time strides in elements."""
+
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_int64), ("time", ctypes.c_int64)]
+
+
+class gs_recurrence(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int64),
+        ("T", ctypes.c_int64),
+        ("C", ctypes.c_int64),
+        ("dtype", ctypes.c_int32),
+        ("x", gs_rows),
+        ("f", gs_rows),
+        ("o", gs_rows),
+        ("lengths", ctypes.c_void_p),
+        ("h0", ctypes.c_void_p),
+    ]
+
+
+class gs_xent(ctypes.Structure):
+    _fields_ = [
+        ("N", ctypes.c_int64),
+        ("V", ctypes.c_int64),
+        ("dtype", ctypes.c_int32),
+        ("mean", ctypes.c_int32),
+        ("logits", ctypes.c_void_p),
+        ("logits_stride", ctypes.c_int64),
+        ("targets", ctypes.c_void_p),
+        ("ignore_index", ctypes.c_int64),
+        ("factor", ctypes.c_float),
+        ("scale", ctypes.c_void_p),
+        ("scale_stride", ctypes.c_int64),
+        ("losses", ctypes.c_void_p),
+        ("mean_loss", ctypes.c_void_p),
+        ("grad", ctypes.c_void_p),
+        ("grad_stride", ctypes.c_int64),
+        ("work", ctypes.c_void_p),
+    ]
+
+
 _lib = None
 
 
@@ -106,10 +154,21 @@ def load_library():
     lib.gs_timing_stop.argtypes = [vp, vp, vp]
     lib.gs_unsketch_topk_static.argtypes = [ctypes.POINTER(gs_config), vp, vp, i64, vp, vp]
     lib.gs_describe.argtypes = [vp, ctypes.POINTER(gs_plan)]
+    lib.gs_recurrence_work.argtypes = [i64, i64, i64, ctypes.c_int32]
+    lib.gs_recurrence_work.restype = i64
+    lib.gs_recurrence_forward.argtypes = [ctypes.POINTER(gs_recurrence), vp, gs_rows, vp, vp, vp]
+    lib.gs_recurrence_backward.argtypes = [ctypes.POINTER(gs_recurrence), vp, gs_rows, vp, vp, gs_rows, gs_rows,
+                                           gs_rows, vp, vp]
+    lib.gs_dropout.argtypes = [vp, ctypes.c_int32, i64, i64, vp, i64, vp, i64, vp, i64, ctypes.c_double,
+                               ctypes.c_uint64, ctypes.c_uint64, vp]
+    lib.gs_cross_entropy_work.argtypes = [i64, i64, ctypes.c_int32]
+    lib.gs_cross_entropy_work.restype = i64
+    lib.gs_cross_entropy.argtypes = [ctypes.POINTER(gs_xent), vp]
     for name in ("gs_create", "gs_destroy", "gs_accumulate", "gs_sketch", "gs_merge", "gs_unsketch_topk",
                  "gs_gather_reset", "gs_step", "gs_heavymix_topk", "gs_step_heavymix", "gs_step_sketch_momentum",
                  "gs_apply_update", "gs_step_profiled", "gs_timing_start", "gs_timing_stop",
-                 "gs_unsketch_topk_static"):
+                 "gs_unsketch_topk_static", "gs_recurrence_forward", "gs_recurrence_backward", "gs_dropout",
+                 "gs_cross_entropy"):
         getattr(lib, name).restype = st
     lib.gs_status_string.argtypes = [st]
     lib.gs_status_string.restype = ctypes.c_char_p
