@@ -331,11 +331,13 @@ typedef struct gs_rows {
  *   lengths   [B] int32 or NULL (all T); values outside [0, T] are taken as the nearer end
  *   h0        [B][C] fp32 or NULL (zero)
  * Errors: GS_ERR_INVALID_ARG (nothing is enqueued) for sizes or strides below zero, an unknown
- * dtype, a NULL array, an array not aligned to its elements; GS_ERR_UNSUPPORTED for B, T or C
- * over 2^31 - 1 or, with T > 1, a time stride over GS_RECURRENCE_MAX_STRIDE. */
+ * dtype, a NULL array, an array not aligned to its elements; GS_ERR_UNSUPPORTED for B or T
+ * over 2^30, C over GS_RECURRENCE_MAX_CHANNELS or, with T > 1, a time stride over
+ * GS_RECURRENCE_MAX_STRIDE. */
 #define GS_RECURRENCE_BLOCK 128
 #define GS_RECURRENCE_BLOCKS(T) (((T) + GS_RECURRENCE_BLOCK - 1) / GS_RECURRENCE_BLOCK)
 #define GS_RECURRENCE_MAX_STRIDE 4194304
+#define GS_RECURRENCE_MAX_CHANNELS 16777216
 typedef struct gs_recurrence {
   int64_t B;
   int64_t T;

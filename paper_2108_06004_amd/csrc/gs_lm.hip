@@ -40,8 +40,8 @@ gs_status check_recurrence(const gs_recurrence* r, const char* call, bool* empty
   if (!r) return refuse(GS_ERR_INVALID_ARG, call, "r is NULL");
   if (r->B < 0 || r->T < 0 || r->C < 0) return refuse(GS_ERR_INVALID_ARG, call, "sizes must not be negative");
   if (!known(r->dtype)) return refuse(GS_ERR_INVALID_ARG, call, "dtype must be GS_F32, GS_BF16 or GS_F16");
-  if (r->B > gs::kMaxExtent || r->T > gs::kMaxExtent || r->C > gs::kMaxExtent)
-    return refuse(GS_ERR_UNSUPPORTED, call, "B, T and C must be at most 2^31 - 1");
+  if (r->B > gs::kMaxSteps || r->T > gs::kMaxSteps || r->C > GS_RECURRENCE_MAX_CHANNELS)
+    return refuse(GS_ERR_UNSUPPORTED, call, "B and T must be at most 2^30, C at most GS_RECURRENCE_MAX_CHANNELS");
   *empty = r->B == 0 || r->C == 0;
   if (*empty) return GS_OK;
   if (!aligned(r->lengths, 4) || !aligned(r->h0, 4))
@@ -79,6 +79,7 @@ extern "C" {
 
 int64_t gs_recurrence_work(int64_t B, int64_t T, int64_t C, int32_t dtype) {
   if (B < 0 || T < 0 || C < 0 || !known(dtype)) return -1;
+  if (B > gs::kMaxSteps || T > gs::kMaxSteps || C > GS_RECURRENCE_MAX_CHANNELS) return -1;
   return gs::recurrence_work(B, T, C, dtype);
 }
 

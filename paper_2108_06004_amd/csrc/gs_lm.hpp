@@ -8,7 +8,8 @@
 
 namespace gs {
 
-constexpr int64_t kMaxExtent = 2147483647;
+constexpr int64_t kMaxExtent = 2147483647;  // rows and logits
+constexpr int64_t kMaxSteps = 1 << 30;       // sequences and their steps
 
 inline int elem_size(int dtype) { return dtype == GS_F32 ? 4 : 2; }
 
