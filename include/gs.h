@@ -304,8 +304,8 @@ gs_status gs_describe(const gs_ctx* ctx, gs_plan* out);
  *   - Arrays must be aligned to their elements. Wider alignment and even sizes only make the
  *     calls faster.
  *   - Calls are independent of each other: they share no memory but their arguments, neither
- *     allocate nor synchronize, and can be captured in a HIP graph. Results are the same bits
- *     on every run.
+ *     allocate nor synchronize, and can be captured in a HIP graph. The same call gives the same
+ *     bits on every run; sizes, strides and alignment choose the order of sums.
  *   - Messages of failing calls: gs_last_error(NULL).
  */
 #define GS_F32 0

@@ -1,89 +1,416 @@
 // k_cross_entropy.hip -- softmax cross-entropy of rows of logits and its gradient (include/gs.h).
 //
-// Plain form: one workgroup a row, which it reads three times (maximum, sum, gradient); a kernel
-// before it counts the rows that count, one after it sums their losses.
+// One pass: a workgroup holds its whole row in registers, CH times 16 bytes a thread, so the logits are
+// read once: maximum, sum of exponentials and gradient come from the registers (the exponential twice,
+// which costs less than keeping fp32 values). Rows too long for that, and few long rows, are split over
+// several workgroups: one kernel reduces each part to (maximum, sum), a second joins them and writes the
+// gradient, reading the logits again.
+//
+// Rows need not be aligned: the elements before the first 16-byte boundary of a row and after its last one
+// (up to seven each) go one to a thread.
 #include "gs_lm.hpp"
 
 namespace gs {
 namespace {
 
-constexpr int kBlock = 256;
 constexpr int kTail = 1024;
+constexpr int kInlineCount = 256;  // rows that every workgroup counts by itself
+constexpr int kPartThreads = 256;
+constexpr int kPartVecs = 8;          // 16-byte pieces a thread takes of a part, at least
+constexpr int kMaxParts = 256;
+constexpr int kRowThreads = 1024;
+constexpr int kRowPieces = 16;  // longest row in registers: 16 pieces of 1,024 threads, 256 KB
+constexpr int kSplitWant = 256;  // workgroups that few long rows are split into
+
+__device__ __forceinline__ float inf() { return __builtin_inff(); }
+
+// e^d for d <= 0 (and NaN).
+__device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
 
 template <int THREADS, typename T, typename F>
 __device__ __forceinline__ T block_reduce(T v, T* lds, F f) {
-  lds[threadIdx.x] = v;
+#pragma unroll
+  for (int n = 32; n > 0; n >>= 1) v = f(v, __shfl_xor(v, n));
+  if (THREADS == 64) return v;
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
   __syncthreads();
-  for (int n = THREADS / 2; n > 0; n >>= 1) {
-    if ((int)threadIdx.x < n) lds[threadIdx.x] = f(lds[threadIdx.x], lds[threadIdx.x + n]);
-    __syncthreads();
-  }
-  const T r = lds[0];
-  __syncthreads();
-  return r;
+  v = lds[0];
+#pragma unroll
+  for (int w = 1; w < THREADS / 64; ++w) v = f(v, lds[w]);
+  return v;
+}
+
+__device__ __forceinline__ float count_of(const gs_xent& x, int lane, int lanes) {
+  int n = 0;
+  for (int64_t i = lane; i < x.N; i += lanes) n += x.targets[i] != x.ignore_index;
+  return (float)n;
 }
 
 __global__ void __launch_bounds__(kTail) k_xent_count(gs_xent x) {
-  __shared__ int64_t lds[kTail];
-  int64_t n = 0;
-  for (int64_t i = threadIdx.x; i < x.N; i += kTail) n += x.targets[i] != x.ignore_index;
-  n = block_reduce<kTail>(n, lds, [](int64_t p, int64_t q) { return p + q; });
-  if (threadIdx.x == 0) *static_cast<float*>(x.work) = 1.0f / (float)(n > 0 ? n : 1);
+  __shared__ float lds[kTail / 64];
+  // counts below 2^24 a thread are whole numbers in fp32; the sum is rounded as a whole
+  const float n = block_reduce<kTail>(count_of(x, threadIdx.x, kTail), lds, [](float p, float q) { return p + q; });
+  if (threadIdx.x == 0) *static_cast<float*>(x.work) = 1.0f / fmaxf(n, 1.0f);
 }
 
 __global__ void __launch_bounds__(kTail) k_xent_mean(gs_xent x) {
-  __shared__ double lds[kTail];
+  __shared__ double lds[kTail / 64];
+  __shared__ float cnt[kTail / 64];
+  const float n = block_reduce<kTail>(count_of(x, threadIdx.x, kTail), cnt, [](float p, float q) { return p + q; });
   double sum = 0.0;
   for (int64_t i = threadIdx.x; i < x.N; i += kTail) sum += x.losses[i];
   sum = block_reduce<kTail>(sum, lds, [](double p, double q) { return p + q; });
-  if (threadIdx.x == 0) *x.mean_loss = (float)(sum * *static_cast<const float*>(x.work));
+  if (threadIdx.x == 0) *x.mean_loss = (float)(sum / fmaxf(n, 1.0f));
+}
+
+// The factor of a row's gradient. Rows few enough are counted here, by the first wave's lanes.
+__device__ __forceinline__ float factor_of(const gs_xent& x, int64_t n) {
+  float m = x.factor;
+  if (x.scale) m *= x.scale[n * x.scale_stride];
+  if (x.mean) {
+    if (x.N <= kInlineCount) {
+      float c = count_of(x, threadIdx.x & 63, 64);
+#pragma unroll
+      for (int d = 32; d > 0; d >>= 1) c += __shfl_xor(c, d);
+      m *= 1.0f / fmaxf(c, 1.0f);
+    } else {
+      m *= *static_cast<const float*>(x.work);
+    }
+  }
+  return m;
+}
+
+// Workgroups are counted over two dimensions of the grid: one holds fewer than 2^32 threads.
+constexpr int64_t kGridX = 1 << 21;
+__device__ __forceinline__ int64_t group_of() { return (int64_t)blockIdx.y * kGridX + blockIdx.x; }
+dim3 grid_of(int64_t groups) {
+  return dim3((unsigned)(groups < kGridX ? groups : kGridX), (unsigned)((groups + kGridX - 1) / kGridX));
 }
 
 template <int DT>
-__global__ void __launch_bounds__(kBlock) k_xent(gs_xent x) {
+struct Row {
   using E = typename Elem<DT>::type;
-  __shared__ float lds[kBlock];
-  const int64_t n = blockIdx.x, t = x.targets[n];
-  const E* z = static_cast<const E*>(x.logits) + n * x.logits_stride;
-  E* grad = x.grad ? static_cast<E*>(x.grad) + n * x.grad_stride : nullptr;
+  static constexpr int N = 16 / (int)sizeof(E);
+  using P = Pack<DT, N>;
+  const E* z;
+  E* grad;
+  int head, vecs, tail;  // elements before the first boundary, 16-byte pieces, elements after the last
+  __device__ __forceinline__ Row(const gs_xent& x, int64_t n) {
+    z = static_cast<const E*>(x.logits) + n * x.logits_stride;
+    grad = x.grad ? static_cast<E*>(x.grad) + n * x.grad_stride : nullptr;
+    const int V = (int)x.V, off = (int)((uintptr_t)z & 15) / (int)sizeof(E);
+    head = off ? N - off : 0;
+    head = head < V ? head : V;
+    vecs = (V - head) / N;
+    tail = V - head - vecs * N;
+  }
+  // The element that thread i < head + tail holds beside its pieces; below zero: none.
+  __device__ __forceinline__ int edge(int i) const {
+    return i < head ? i : i < head + tail ? head + vecs * N + (i - head) : -1;
+  }
+  __device__ __forceinline__ typename P::raw get(int j) const {
+    return *reinterpret_cast<const typename P::raw*>(z + head + (int64_t)j * N);
+  }
+  // Gradients need not have the logits' alignment.
+  template <bool SAME>
+  __device__ __forceinline__ void put(int j, typename P::raw v) const {
+    E* g = grad + head + (int64_t)j * N;
+    if (SAME) {
+      *reinterpret_cast<typename P::raw*>(g) = v;
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e) g[e] = v[e];
+    }
+  }
+  // A piece of the gradient m (softmax - [v = t]); `at` is t - head.
+  template <bool SAME>
+  __device__ __forceinline__ void put_grad(int j, typename P::raw r, float top, float share, float m, int at) const {
+    typename P::wide v = P::up(r);
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = exp_of(v[e] - top) * share;
+    if (at >= 0 && at / N == j) {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (e == at % N) v[e] -= 1.0f;
+    }
+    put<SAME>(j, P::down(v * m));
+  }
+};
+
+// Keeps the compiler from holding a piece's fp32 form from one pass over the registers to the next (twice
+// the registers): converting again is cheap.
+template <typename T>
+__device__ __forceinline__ void as_stored(T& v) {
+  static_assert(sizeof(T) == 16, "a 16-byte piece");
+  typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+  u4 w = __builtin_bit_cast(u4, v);
+  asm volatile("" : "+v"(w));
+  v = __builtin_bit_cast(T, w);
+}
+
+template <int DT, int THREADS, int CH, bool GRAD, bool SAME>
+__global__ void __launch_bounds__(THREADS) k_xent_row(gs_xent x) {
+  using R = Row<DT>;
+  using P = typename R::P;
+  using E = typename R::E;
+  __shared__ float lds_top[THREADS / 64], lds_sum[THREADS / 64];
+  const int64_t n = group_of();
+  if (n >= x.N) return;
+  const int64_t t = x.targets[n];
+  const R row(x, n);
+  const int tid = threadIdx.x, edge = row.edge(tid);
   if (t == x.ignore_index) {
-    if (threadIdx.x == 0 && x.losses) x.losses[n] = 0.0f;
-    if (grad)
-      for (int64_t v = threadIdx.x; v < x.V; v += kBlock) grad[v] = (E)0.0f;
+    if (tid == 0 && x.losses) x.losses[n] = 0.0f;
+    if (GRAD) {
+      for (int j = tid; j < row.vecs; j += THREADS) row.template put<SAME>(j, P::down((typename P::wide)0.0f));
+      if (edge >= 0) row.grad[edge] = (E)0.0f;
+    }
     return;
   }
-  const bool known = t >= 0 && t < x.V;
-  const float at = known ? (float)z[t] : __builtin_nanf("");
-  float top = -__builtin_inff();
-  for (int64_t v = threadIdx.x; v < x.V; v += kBlock) top = fmaxf(top, (float)z[v]);
-  top = block_reduce<kBlock>(top, lds, [](float p, float q) { return fmaxf(p, q); });
-  float sum = 0.0f;
-  for (int64_t v = threadIdx.x; v < x.V; v += kBlock) sum += __builtin_amdgcn_exp2f(((float)z[v] - top) * kLog2e);
-  sum = block_reduce<kBlock>(sum, lds, [](float p, float q) { return p + q; });
-  if (threadIdx.x == 0 && x.losses) x.losses[n] = logf(sum) - (at - top);
-  if (!grad) return;
-  float m = x.factor;
-  if (x.scale) m *= x.scale[n * x.scale_stride];
-  if (x.mean) m *= *static_cast<const float*>(x.work);
-  const float share = known ? 1.0f / sum : __builtin_nanf("");
-  for (int64_t v = threadIdx.x; v < x.V; v += kBlock) {
-    const float p = __builtin_amdgcn_exp2f(((float)z[v] - top) * kLog2e) * share;
-    grad[v] = (E)(m * (v == t ? p - 1.0f : p));
+  typename P::raw r[CH];
+#pragma unroll
+  for (int i = 0; i < CH; ++i) {
+    const int j = tid + i * THREADS;
+    if (j < row.vecs)
+      r[i] = row.get(j);
+    else
+      r[i] = P::down((typename P::wide)(-inf()));
   }
+  const float side = edge >= 0 ? (float)row.z[edge] : -inf();
+  const bool known = t >= 0 && t < x.V;
+  const float at = known ? (float)row.z[t] : __builtin_nanf("");
+  const float m = GRAD ? factor_of(x, n) : 0.0f;
+  float top = side;
+#pragma unroll
+  for (int i = 0; i < CH; ++i)
+    if (i * THREADS < row.vecs) {
+      const typename P::wide v = P::up(r[i]);
+#pragma unroll
+      for (int e = 0; e < R::N; ++e) top = fmaxf(top, v[e]);
+    }
+  top = block_reduce<THREADS>(top, lds_top, [](float p, float q) { return fmaxf(p, q); });
+  float sum = edge >= 0 ? exp_of(side - top) : 0.0f;
+#pragma unroll
+  for (int i = 0; i < CH; ++i)
+    if (i * THREADS < row.vecs) {
+      as_stored(r[i]);
+      const typename P::wide v = P::up(r[i]);
+#pragma unroll
+      for (int e = 0; e < R::N; ++e) sum += exp_of(v[e] - top);
+    }
+  sum = block_reduce<THREADS>(sum, lds_sum, [](float p, float q) { return p + q; });
+  if (tid == 0 && x.losses) x.losses[n] = logf(sum) - (at - top);
+  if (!GRAD) return;
+  const float share = known ? 1.0f / sum : __builtin_nanf("");
+  const int mark = known ? (int)t - row.head : -1;
+#pragma unroll
+  for (int i = 0; i < CH; ++i) {
+    const int j = tid + i * THREADS;
+    as_stored(r[i]);
+    if (j < row.vecs) row.template put_grad<SAME>(j, r[i], top, share, m, mark);
+  }
+  if (edge >= 0) {
+    const float p = exp_of(side - top) * share;
+    row.grad[edge] = (E)(m * (known && edge == (int)t ? p - 1.0f : p));
+  }
+}
+
+// (maximum, sum of e^(z - maximum)) of what has been seen; a maximum of -inf stands for 0 in the sum.
+struct Seen {
+  float top, sum;
+};
+
+__device__ __forceinline__ float base_of(float top) { return top == -inf() ? 0.0f : top; }
+
+// A side that has seen nothing (or only -inf, or NaN) keeps its sum, 0 or NaN, as it is.
+__device__ __forceinline__ float moved(Seen p, float top) { return p.top == -inf() ? p.sum : p.sum * exp_of(p.top - top); }
+
+__device__ __forceinline__ Seen join(Seen p, Seen q) {
+  const float top = fmaxf(p.top, q.top);
+  return Seen{top, moved(p, top) + moved(q, top)};
+}
+
+// Work: one float (1 / rows that count) and one unused, the targets' logits [N], the parts [N][parts].
+__device__ __forceinline__ float* targets_of(const gs_xent& x) { return static_cast<float*>(x.work) + 2; }
+__device__ __forceinline__ Seen* parts_of(const gs_xent& x, int64_t n, int parts) {
+  return reinterpret_cast<Seen*>(static_cast<float*>(x.work) + 2 + (x.N + 1) / 2 * 2) + n * parts;
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kPartThreads) k_xent_part(gs_xent x, int parts, int part_vecs) {
+  using R = Row<DT>;
+  using P = typename R::P;
+  __shared__ Seen lds[kPartThreads / 64];
+  const int64_t id = group_of(), n = id / parts;
+  if (n >= x.N) return;
+  const int64_t t = x.targets[n];
+  if (t == x.ignore_index) return;
+  const int part = (int)(id - n * parts), tid = threadIdx.x;
+  const R row(x, n);
+  const int from = part * part_vecs, to = from + part_vecs < row.vecs ? from + part_vecs : row.vecs;
+  Seen mine{-inf(), 0.0f};
+  if (part == 0) {
+    if (tid == 0) targets_of(x)[n] = t >= 0 && t < x.V ? (float)row.z[t] : __builtin_nanf("");
+    const int edge = row.edge(tid);
+    if (edge >= 0) {
+      const float z = (float)row.z[edge];
+      mine = Seen{fmaxf(z, -inf()), exp_of(z - base_of(fmaxf(z, -inf())))};
+    }
+  }
+  constexpr int U = 4;
+  for (int j0 = from + tid; j0 < to; j0 += U * kPartThreads) {
+    typename P::raw r[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int j = j0 + u * kPartThreads;
+      if (j < to)
+        r[u] = row.get(j);
+      else
+        r[u] = P::down((typename P::wide)(-inf()));
+    }
+    Seen now{-inf(), 0.0f};
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const typename P::wide v = P::up(r[u]);
+#pragma unroll
+      for (int e = 0; e < R::N; ++e) now.top = fmaxf(now.top, v[e]);
+    }
+    const float b = base_of(now.top);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const typename P::wide v = P::up(r[u]);
+#pragma unroll
+      for (int e = 0; e < R::N; ++e) now.sum += exp_of(v[e] - b);
+    }
+    mine = join(mine, now);
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) mine = join(mine, Seen{__shfl_xor(mine.top, d), __shfl_xor(mine.sum, d)});
+  if ((tid & 63) == 0) lds[tid >> 6] = mine;
+  __syncthreads();
+  if (tid == 0) {
+    Seen all = lds[0];
+#pragma unroll
+    for (int w = 1; w < kPartThreads / 64; ++w) all = join(all, lds[w]);
+    parts_of(x, n, parts)[part] = all;
+  }
+}
+
+// Joins a row's parts (every workgroup, in one order) and writes the gradient of one of them. Without a
+// gradient there is one workgroup a row.
+template <int DT, bool GRAD, bool SAME>
+__global__ void __launch_bounds__(kPartThreads) k_xent_join(gs_xent x, int parts, int part_vecs) {
+  using R = Row<DT>;
+  using P = typename R::P;
+  using E = typename R::E;
+  const int64_t id = group_of(), n = GRAD ? id / parts : id;
+  if (n >= x.N) return;
+  const int64_t t = x.targets[n];
+  const int part = GRAD ? (int)(id - n * parts) : 0, tid = threadIdx.x;
+  const R row(x, n);
+  const int from = part * part_vecs, to = from + part_vecs < row.vecs ? from + part_vecs : row.vecs;
+  const int edge = part == 0 ? row.edge(tid) : -1;
+  if (t == x.ignore_index) {
+    if (part == 0 && tid == 0 && x.losses) x.losses[n] = 0.0f;
+    if (GRAD) {
+      for (int j = from + tid; j < to; j += kPartThreads)
+        row.template put<SAME>(j, P::down((typename P::wide)0.0f));
+      if (edge >= 0) row.grad[edge] = (E)0.0f;
+    }
+    return;
+  }
+  const Seen* all = parts_of(x, n, parts);
+  Seen s = all[0];
+  for (int q = 1; q < parts; ++q) s = join(s, all[q]);
+  if (part == 0 && tid == 0 && x.losses) x.losses[n] = logf(s.sum) - (targets_of(x)[n] - s.top);
+  if (!GRAD) return;
+  const bool known = t >= 0 && t < x.V;
+  const float share = known ? 1.0f / s.sum : __builtin_nanf(""), m = factor_of(x, n);
+  const int mark = known ? (int)t - row.head : -1;
+  for (int j = from + tid; j < to; j += kPartThreads)
+    row.template put_grad<SAME>(j, row.get(j), s.top, share, m, mark);
+  if (edge >= 0) {
+    const float p = exp_of((float)row.z[edge] - s.top) * share;
+    row.grad[edge] = (E)(m * (known && edge == (int)t ? p - 1.0f : p));
+  }
+}
+
+// How a row is worked on: parts > 0: split.
+struct Cut {
+  int parts, part_vecs;
+};
+
+Cut cut_of(int64_t N, int64_t V, int dtype) {
+  const int64_t vecs = V / (16 / elem_size(dtype)) + 1;
+  const bool held = vecs <= (int64_t)kRowThreads * kRowPieces;
+  const int64_t least = kPartThreads * kPartVecs;
+  int64_t parts = 0;
+  if (!held || (N * 4 <= kSplitWant && vecs >= 4 * least)) {
+    parts = N > 0 ? (kSplitWant + N - 1) / N : 1;
+    const int64_t most = (vecs + least - 1) / least;
+    parts = parts < most ? parts : most;
+    parts = parts < kMaxParts ? parts : kMaxParts;
+    parts = parts > 1 ? parts : 1;
+  }
+  Cut k{(int)parts, 0};
+  if (parts > 0) k.part_vecs = (int)((vecs + parts - 1) / parts);
+  return k;
+}
+
+template <int DT, bool GRAD, bool SAME>
+void rows(hipStream_t s, const gs_xent& x) {
+  const int64_t vecs = x.V / (16 / elem_size(DT)) + 1;
+  const dim3 grid = grid_of(x.N);
+#define GS_XENT(THREADS, CH) \
+  if (vecs <= (THREADS) * (CH)) return k_xent_row<DT, THREADS, CH, GRAD, SAME><<<grid, THREADS, 0, s>>>(x), void()
+  GS_XENT(64, 1);
+  GS_XENT(64, 2);
+  GS_XENT(64, 4);
+  GS_XENT(256, 2);
+  GS_XENT(256, 4);
+  GS_XENT(256, 8);
+  GS_XENT(512, 6);
+  GS_XENT(512, 8);
+  GS_XENT(1024, 8);
+  GS_XENT(kRowThreads, kRowPieces);
+#undef GS_XENT
+}
+
+template <int DT, bool GRAD, bool SAME>
+void launch(hipStream_t s, const gs_xent& x) {
+  const Cut k = cut_of(x.N, x.V, DT);
+  if (k.parts == 0) return rows<DT, GRAD, SAME>(s, x);
+  const dim3 grid = grid_of(x.N * k.parts);
+  k_xent_part<DT><<<grid, kPartThreads, 0, s>>>(x, k.parts, k.part_vecs);
+  k_xent_join<DT, GRAD, SAME><<<GRAD ? grid : grid_of(x.N), kPartThreads, 0, s>>>(x, k.parts, k.part_vecs);
+}
+
+template <int DT>
+void launch(hipStream_t s, const gs_xent& x) {
+  const int64_t bytes = elem_size(DT);
+  const bool same = x.grad && (((uintptr_t)x.grad - (uintptr_t)x.logits) & 15) == 0 &&
+                    (x.N == 1 || ((x.grad_stride - x.logits_stride) * bytes & 15) == 0);
+  if (!x.grad)
+    launch<DT, false, true>(s, x);
+  else if (same)
+    launch<DT, true, true>(s, x);
+  else
+    launch<DT, true, false>(s, x);
 }
 
 }  // namespace
 
-int64_t cross_entropy_work(int64_t, int64_t, int) { return 8; }
+int64_t cross_entropy_work(int64_t N, int64_t V, int dtype) {
+  const Cut k = cut_of(N, V, dtype);
+  return 8 + (k.parts ? (N + 1) / 2 * 8 + N * k.parts * (int64_t)sizeof(Seen) : 0);
+}
 
 hipError_t launch_cross_entropy(hipStream_t s, const gs_xent& x) {
-  if (x.N == 0 && !x.mean_loss) return hipSuccess;
-  if (x.mean_loss || (x.mean && x.grad)) k_xent_count<<<1, kTail, 0, s>>>(x);
   if (x.N > 0) {
-    const dim3 grid((unsigned)x.N);
-    if (x.dtype == GS_F32) k_xent<GS_F32><<<grid, kBlock, 0, s>>>(x);
-    if (x.dtype == GS_BF16) k_xent<GS_BF16><<<grid, kBlock, 0, s>>>(x);
-    if (x.dtype == GS_F16) k_xent<GS_F16><<<grid, kBlock, 0, s>>>(x);
+    if (x.mean && x.grad && x.N > kInlineCount) k_xent_count<<<1, kTail, 0, s>>>(x);
+    if (x.dtype == GS_F32) launch<GS_F32>(s, x);
+    if (x.dtype == GS_BF16) launch<GS_BF16>(s, x);
+    if (x.dtype == GS_F16) launch<GS_F16>(s, x);
   }
   if (x.mean_loss) k_xent_mean<<<1, kTail, 0, s>>>(x);
   return hipGetLastError();

@@ -366,7 +366,9 @@ def check_xent(z, t, ignore=-100, what=""):
     ref.check(grad, want["grad"], z.dtype, what + " grad")
     inside = z.clone()
     lm.cross_entropy_forward(inside, t, ignore, grad=inside)
-    assert torch.equal(inside, grad), what + " in place"
+    ref.check(inside, want["grad"], z.dtype, what + " in place")
+    if inside.stride() == z.stride():  # the bits of a row depend on its alignment
+        assert torch.equal(inside, grad), what + " in place"
     return grad
 
 
@@ -459,7 +461,8 @@ def test_cross_entropy_offsets_beyond_32_bits():
     store = torch.empty(stride + V, dtype=torch.bfloat16, device=DEV)
     view = store.as_strided((N, V), (stride, 1))
     view.copy_(z)
-    assert torch.equal(lm.cross_entropy_forward(view, t, grad=True)[2], check_xent(z, t))
+    check_xent(z, t)
+    ref.check(lm.cross_entropy_forward(view, t, grad=True)[2], ref.cross_entropy(z, t)["grad"], torch.bfloat16, "far rows")
 
 
 def test_cross_entropy_gradient_against_differences():
