@@ -351,8 +351,8 @@ typedef struct gs_recurrence {
 } gs_recurrence;
 
 /* Bytes of the `work` scratch of the two calls below at these sizes, for either direction
- * (0: none is needed and work may be NULL; negative: sizes below zero or an unknown dtype). Its
- * contents need not be set and are not kept for anything. */
+ * (0, always up to T = GS_RECURRENCE_BLOCK: none is needed and work may be NULL; negative: sizes out
+ * of range or an unknown dtype). Its contents need not be set and are not kept for anything. */
 int64_t gs_recurrence_work(int64_t B, int64_t T, int64_t C, int32_t dtype);
 
 /* Forward. y: [B][T][C] output. h_last: [B][C] fp32 output, the state after each sequence's last

@@ -402,10 +402,12 @@ void launch(hipStream_t s, const gs_xent& x) {
 
 int64_t cross_entropy_work(int64_t N, int64_t V, int dtype) {
   const Cut k = cut_of(N, V, dtype);
+  if (k.parts == 0 && N <= kInlineCount) return 0;
   return 8 + (k.parts ? (N + 1) / 2 * 8 + N * k.parts * (int64_t)sizeof(Seen) : 0);
 }
 
 hipError_t launch_cross_entropy(hipStream_t s, const gs_xent& x) {
+  if (x.N == 0 && !x.mean_loss) return hipSuccess;
   if (x.N > 0) {
     if (x.mean && x.grad && x.N > kInlineCount) k_xent_count<<<1, kTail, 0, s>>>(x);
     if (x.dtype == GS_F32) launch<GS_F32>(s, x);

@@ -23,32 +23,45 @@ import ctypes
 
 import torch
 
-from . import (GS_BF16, GS_F16, GS_F32, GS_RECURRENCE_BLOCK, _check, _ptr, _stream, gs_recurrence, gs_rows, gs_xent,
+from . import (GS_BF16, GS_F16, GS_F32, GS_RECURRENCE_BLOCK, _check, gs_recurrence, gs_rows, gs_xent,
                load_library)
 
 DTYPES = {torch.float32: GS_F32, torch.bfloat16: GS_BF16, torch.float16: GS_F16}
 U64 = (1 << 64) - 1
 
 
-def _activation(t, name: str, dim: int | None = None) -> int:
-    """The C ABI's type code of an activation tensor after its checks."""
+def _current_stream() -> int:
+    return torch.cuda.current_stream().cuda_stream
+
+
+# the stream's handle without a Stream object around it (2.7 us a call less), where torch has it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream(device: int) -> int:
+    return _raw_stream(device) if _raw_stream is not None else _current_stream()
+
+
+def _activation(t, name: str, dim: int | None = None) -> tuple[int, int]:
+    """(the C ABI's type code, the device) of an activation tensor, after its checks."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
     code = DTYPES.get(t.dtype)
     if code is None:
         raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
-    if t.get_device() != torch.cuda.current_device():
+    device = t.get_device()
+    if device != torch.cuda.current_device():
         raise ValueError(f"{name} must be on the current device")
     if dim is not None and t.dim() != dim:
         raise ValueError(f"{name} must have {dim} dimensions, got {t.dim()}")
-    return code
+    return code, device
 
 
-def _rows(t, like, name: str) -> gs_rows:
+def _rows(t, like, device: int, name: str) -> gs_rows:
     """A [B][T][C] tensor whose channels are contiguous, as the C ABI takes it."""
     if t is None:
         return gs_rows(None, 0, 0)
-    if not isinstance(t, torch.Tensor) or t.device != like.device or t.dtype != like.dtype:
+    if not isinstance(t, torch.Tensor) or t.get_device() != device or t.dtype is not like.dtype:
         raise TypeError(f"{name} must be a {like.dtype} tensor on {like.device}")
     if t.shape != like.shape:
         raise ValueError(f"{name} must have shape {tuple(like.shape)}, got {tuple(t.shape)}")
@@ -65,26 +78,28 @@ def _written(t, name: str) -> None:
             raise ValueError(f"{name} must not be an expanded tensor")
 
 
-def _recurrence(x, f, o, h0, lengths):
-    code = _activation(x, "x", 3)
-    B, T, C = x.shape
-    r = gs_recurrence(B, T, C, code, _rows(x, x, "x"), _rows(f, x, "f"), _rows(o, x, "o"),
-                      _side(lengths, torch.int32, (B,), x, "lengths"), _side(h0, torch.float32, (B, C), x, "h0"))
-    return r, code
-
-
-def _side(t, dtype, shape, like, name: str):
+def _side(t, dtype, shape, device: int, name: str):
+    """The pointer of a contiguous tensor of the given type and shape on `device` (None: NULL)."""
     if t is None:
         return None
-    p = _ptr(t, dtype, None, name)
-    if t.shape != shape or t.device != like.device:
-        raise ValueError(f"{name} must have shape {shape} on {like.device}, got {tuple(t.shape)} on {t.device}")
-    return p
+    if not isinstance(t, torch.Tensor) or t.get_device() != device or t.dtype is not dtype:
+        raise TypeError(f"{name} must be a {dtype} tensor on cuda:{device}")
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous, of shape {shape}, got {tuple(t.shape)}")
+    return t.data_ptr()
 
 
-def _recurrence_scratch(lib, x, code):
-    n = lib.gs_recurrence_work(x.shape[0], x.shape[1], x.shape[2], code)
-    return torch.empty(n, dtype=torch.uint8, device=x.device) if n > 0 else None
+def _recurrence(x, f, o, h0, lengths):
+    code, device = _activation(x, "x", 3)
+    B, T, C = x.shape
+    r = gs_recurrence(B, T, C, code, _rows(x, x, device, "x"), _rows(f, x, device, "f"), _rows(o, x, device, "o"),
+                      _side(lengths, torch.int32, (B,), device, "lengths"),
+                      _side(h0, torch.float32, (B, C), device, "h0"))
+    work = None
+    if T > GS_RECURRENCE_BLOCK:
+        n = load_library().gs_recurrence_work(B, T, C, code)
+        work = torch.empty(n, dtype=torch.uint8, device=x.device) if n > 0 else None
+    return r, device, work
 
 
 def recurrence_forward(x, f, o=None, h0=None, lengths=None, save: bool = False, y=None, h_last=None):
@@ -94,11 +109,10 @@ def recurrence_forward(x, f, o=None, h0=None, lengths=None, save: bool = False, 
     None: y is the state). h0: [B][C] fp32 or None (zero). lengths: int32 [B] or None; positions from
     a sequence's length on are padding: they keep its state and give y = 0. y and h_last ([B][C] fp32, h0
     itself for a step in place) are made unless given. save: also the states that ``recurrence_backward`` needs."""
-    lib = load_library()
-    r, code = _recurrence(x, f, o, h0, lengths)
+    r, device, work = _recurrence(x, f, o, h0, lengths)
     B, T, C = x.shape
     if y is None:
-        y = torch.empty((B, T, C), dtype=x.dtype, device=x.device)
+        y = torch.empty_like(x, memory_format=torch.contiguous_format)
     else:
         _written(y, "y")
     if h_last is None:
@@ -106,10 +120,10 @@ def recurrence_forward(x, f, o=None, h0=None, lengths=None, save: bool = False, 
     saved = None
     if save:
         saved = torch.empty((B, -(-T // GS_RECURRENCE_BLOCK), C), dtype=torch.float32, device=x.device)
-    work = _recurrence_scratch(lib, x, code)
-    _check(lib.gs_recurrence_forward(ctypes.byref(r), _stream(None), _rows(y, x, "y"),
-                                     _side(h_last, torch.float32, (B, C), x, "h_last"),
-                                     saved.data_ptr() if save else None, work.data_ptr() if work is not None else None),
+    _check(load_library().gs_recurrence_forward(ctypes.byref(r), _stream(device), _rows(y, x, device, "y"),
+                                                _side(h_last, torch.float32, (B, C), device, "h_last"),
+                                                saved.data_ptr() if save else None,
+                                                work.data_ptr() if work is not None else None),
            None, "gs_recurrence_forward")
     return y, h_last, saved
 
@@ -118,13 +132,12 @@ def recurrence_backward(gy, x, f, o, saved, lengths=None, gh=None, dx=None, df=N
     """The gradients ``(dx, df, do, dh0)`` of the recurrence. gy: [B][T][C], the gradient of y; gh:
     [B][C] fp32, that of h_last, or None; saved: the forward call's, on the same inputs. dx, df and do are
     made unless given (do is None without o)."""
-    lib = load_library()
-    r, code = _recurrence(x, f, o, None, lengths)
+    r, device, work = _recurrence(x, f, o, None, lengths)
     B, T, C = x.shape
 
     def out(t, name):
         if t is None:
-            return torch.empty((B, T, C), dtype=x.dtype, device=x.device)
+            return torch.empty_like(x, memory_format=torch.contiguous_format)
         _written(t, name)
         return t
 
@@ -133,13 +146,13 @@ def recurrence_backward(gy, x, f, o, saved, lengths=None, gh=None, dx=None, df=N
         raise ValueError("do is given but o is not")
     do = out(do, "do") if o is not None else None
     dh0 = torch.empty((B, C), dtype=torch.float32, device=x.device)
-    work = _recurrence_scratch(lib, x, code)
     blocks = -(-T // GS_RECURRENCE_BLOCK)
-    _check(lib.gs_recurrence_backward(ctypes.byref(r), _stream(None), _rows(gy, x, "gy"),
-                                      _side(gh, torch.float32, (B, C), x, "gh"),
-                                      _side(saved, torch.float32, (B, blocks, C), x, "saved"), _rows(dx, x, "dx"),
-                                      _rows(df, x, "df"), _rows(do, x, "do"), dh0.data_ptr(),
-                                      work.data_ptr() if work is not None else None),
+    _check(load_library().gs_recurrence_backward(ctypes.byref(r), _stream(device), _rows(gy, x, device, "gy"),
+                                                 _side(gh, torch.float32, (B, C), device, "gh"),
+                                                 _side(saved, torch.float32, (B, blocks, C), device, "saved"),
+                                                 _rows(dx, x, device, "dx"), _rows(df, x, device, "df"),
+                                                 _rows(do, x, device, "do"), dh0.data_ptr(),
+                                                 work.data_ptr() if work is not None else None),
            None, "gs_recurrence_backward")
     return dx, df, do, dh0
 
@@ -209,32 +222,26 @@ def _like(t, x, name: str) -> None:
 
 
 def _dropout(x, p, seed, site, step, residual, y):
-    lib = load_library()
-    code = _activation(x, "x")
+    code, device = _activation(x, "x")
     if residual is not None:
         _like(residual, x, "residual")
     if y is None:
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        y = torch.empty_like(x, memory_format=torch.contiguous_format)
     else:
         _like(y, x, "y")
         _written(y, "y")
-    used = [t for t in (x, residual, y) if t is not None]
-    if all(t.is_contiguous() for t in used):
+    if x.is_contiguous() and y.is_contiguous() and (residual is None or residual.is_contiguous()):
         rows, cols = 1, x.numel()
         xs = rs = ys = cols
     else:
-        if x.dim() != 2 or any(t.stride(1) != 1 and t.shape[1] > 1 for t in used):
+        if x.dim() != 2 or any(t.stride(1) != 1 and t.shape[1] > 1 for t in (x, residual, y) if t is not None):
             raise ValueError("x, residual and y must be contiguous, or two-dimensional with contiguous rows")
         rows, cols = x.shape
         xs, ys, rs = x.stride(0), y.stride(0), residual.stride(0) if residual is not None else 0
-    sp = None
-    if step is not None:
-        sp = _ptr(step, torch.int64, 1, "step")
-        if step.device != x.device:
-            raise ValueError(f"step must be on {x.device}")
-    _check(lib.gs_dropout(_stream(None), code, rows, cols, x.data_ptr(), xs,
-                          residual.data_ptr() if residual is not None else None, rs, y.data_ptr(), ys, p, seed & U64,
-                          site & U64, sp), None, "gs_dropout")
+    _check(load_library().gs_dropout(_stream(device), code, rows, cols, x.data_ptr(), xs,
+                                     residual.data_ptr() if residual is not None else None, rs, y.data_ptr(), ys, p,
+                                     seed & U64, site & U64, _side(step, torch.int64, (1,), device, "step")),
+           None, "gs_dropout")
     return y
 
 
@@ -275,27 +282,27 @@ def dropout(x, p: float, seed: int, site: int = 0, step=None, residual=None):
 
 def _cross_entropy(logits, targets, ignore_index, losses, mean_loss, grad, factor=1.0, scale=None, mean=False):
     lib = load_library()
-    code = _activation(logits, "logits", 2)
+    code, device = _activation(logits, "logits", 2)
     N, V = logits.shape
     if logits.stride(1) != 1 and V > 1:
         raise ValueError("logits: rows must be contiguous")
-    tp = _side(targets, torch.int64, (N,), logits, "targets")
+    grad_stride = V
     if grad is not None:
         _like(grad, logits, "grad")
+        grad_stride = grad.stride(0)
         if grad.stride(1) != 1 and V > 1:
             raise ValueError("grad: rows must be contiguous")
     n = lib.gs_cross_entropy_work(N, V, code)
     work = torch.empty(n // 8, dtype=torch.int64, device=logits.device) if n > 0 else None
-    per_row = 0
-    if scale is not None:
-        per_row = int(scale.dim() == 1)
-        scale = _side(scale, torch.float32, (N,) if per_row else (), logits, "scale")
-    x = gs_xent(N, V, code, int(mean), logits.data_ptr(), logits.stride(0), tp, ignore_index, factor, scale, per_row,
+    per_row = int(scale is not None and scale.dim() == 1)
+    x = gs_xent(N, V, code, mean, logits.data_ptr(), logits.stride(0),
+                _side(targets, torch.int64, (N,), device, "targets"), ignore_index, factor,
+                _side(scale, torch.float32, (N,) if per_row else (), device, "scale"), per_row,
                 losses.data_ptr() if losses is not None else None,
                 mean_loss.data_ptr() if mean_loss is not None else None,
-                grad.data_ptr() if grad is not None else None, grad.stride(0) if grad is not None else V,
+                grad.data_ptr() if grad is not None else None, grad_stride,
                 work.data_ptr() if work is not None else None)
-    _check(lib.gs_cross_entropy(ctypes.byref(x), _stream(None)), None, "gs_cross_entropy")
+    _check(lib.gs_cross_entropy(ctypes.byref(x), _stream(device)), None, "gs_cross_entropy")
 
 
 def cross_entropy_forward(logits, targets, ignore_index: int = -100, grad=False, factor: float = 1.0):
