@@ -334,7 +334,7 @@ typedef struct gs_rows {
  * dtype, a NULL array, an array not aligned to its elements; GS_ERR_UNSUPPORTED for B or T
  * over 2^30, C over GS_RECURRENCE_MAX_CHANNELS or, with T > 1, a time stride over
  * GS_RECURRENCE_MAX_STRIDE. */
-#define GS_RECURRENCE_BLOCK 128
+#define GS_RECURRENCE_BLOCK 32
 #define GS_RECURRENCE_BLOCKS(T) (((T) + GS_RECURRENCE_BLOCK - 1) / GS_RECURRENCE_BLOCK)
 #define GS_RECURRENCE_MAX_STRIDE 4194304
 #define GS_RECURRENCE_MAX_CHANNELS 16777216

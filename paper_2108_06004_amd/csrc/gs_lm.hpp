@@ -49,6 +49,10 @@ __device__ __forceinline__ void sigmoid_both(float z, float& s, float& rest) {
   rest = z >= 0.0f ? small : big;
 }
 
+__device__ __forceinline__ float sigmoid_of(float z) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-z * kLog2e));
+}
+
 // A [B][T][C] array with its strides in bytes.
 struct Rows {
   char* p;

@@ -6,15 +6,15 @@
 // three times:
 //   - a thread takes L consecutive steps of VEC neighbouring channels. Their loads are all in flight
 //     together (L for each array); it forms its own (A, S) in registers;
-//   - a workgroup of W x G threads takes a strip of W VEC channels and a block of G L = 128 steps. The
-//     groups' maps go through LDS, every thread joins those before its own and runs its steps
+//   - a workgroup of W x G threads takes a strip of W VEC channels and a block of G L = 64 steps, a wave
+//     L of them. The waves' maps go through LDS, every thread joins those before its own and runs its steps
 //     again from registers with the true state. One barrier a block: the maps have two buffers;
 //   - where B and C give too few workgroups, `segs` workgroups share a sequence's blocks. A first
 //     kernel reduces each segment to its map (reading x and f once more), the second starts each segment
 //     from the joined maps before it.
 // The backward pass runs the blocks from the last to the first. s_t = q_t + a_(t+1) s_(t+1) is the
 // same recurrence in reverse, carried as c_t = a_t s_t with the map c -> A c + R; the states are computed
-// again from the state before each block that the forward pass saved (4 / 128 bytes a step).
+// again from the state before each block that the forward pass saved (4 / 64 bytes a step).
 #include <type_traits>
 
 #include "gs_lm.hpp"
@@ -22,56 +22,96 @@
 namespace gs {
 namespace {
 
-constexpr int kWantGroups = 512;            // workgroups that fill the chip: two a CU
-constexpr int kMaxSegs = 128;
-constexpr int kGridY = 32768;
+constexpr unsigned kGridX = 1u << 22;  // a grid's first dimension holds fewer than 2^32 threads
 
-__device__ __forceinline__ int64_t length_of(const RecurrenceArgs& a, int64_t b) {
-  if (!a.lengths) return a.T;
-  const int64_t n = a.lengths[b];
-  return n < 0 ? 0 : n > a.T ? a.T : n;
+// The tokens of a sequence, in a scalar register: what follows from it (blocks, buffers) is the same for the
+// whole workgroup, and the compiler has to see that.
+__device__ __forceinline__ int length_of(const RecurrenceArgs& a, int64_t b) {
+  const int T = (int)a.T;
+  const int n = a.lengths ? __builtin_amdgcn_readfirstlane(a.lengths[b]) : T;
+  return n < 0 ? 0 : n > T ? T : n;
 }
 
 // How a launch cuts the problem: `strips` of channels x `segs` of blocks x sequences.
 struct Cut {
   unsigned strips;
-  int segs;
-  int64_t blocks, seg_blocks;
+  int segs, groups;
+  int blocks, all, seg_blocks;  // saved states of a sequence; the workgroups' own blocks, all and a segment's
 };
 
-// Where one workgroup is; a reducing backward kernel leaves out segment 0.
+// Where one workgroup is; a reducing kernel leaves out the last segment, or going backward the first (from = 1).
 struct Place {
-  int64_t b, blk0, blk1;
+  int64_t b;
   unsigned strip;
-  int seg;
+  int seg, blk0, blk1;
 };
 
-__device__ __forceinline__ Place place_of(const Cut& k, int from) {
+// Workgroups go to the eight XCDs in turn, and each XCD has its own L2. Rows that are no multiple of 128 bytes
+// share lines between neighbouring strips, so all strips of a sequence's segment go to one XCD, one after the
+// other (NEAR; what is left over past a multiple of eight segments goes as it comes).
+template <bool NEAR>
+__device__ __forceinline__ Place place_of(const Cut& k, unsigned parts, int from, int64_t B) {
+  const unsigned id = blockIdx.y * kGridX + blockIdx.x;
+  const unsigned even = NEAR ? (unsigned)B * parts / 8 * 8 : 0;
   Place p;
-  const unsigned part = blockIdx.x / k.strips;
-  p.strip = blockIdx.x - part * k.strips;
-  p.seg = (int)part + from;
-  p.b = (int64_t)blockIdx.z * kGridY + blockIdx.y;
+  unsigned item;
+  if (NEAR && id < even * k.strips) {
+    const unsigned slot = id / 8;
+    item = slot / k.strips;
+    p.strip = slot - item * k.strips;
+    item = item * 8 + id % 8;
+  } else {
+    const unsigned left = id - even * k.strips;
+    item = left / k.strips;
+    p.strip = left - item * k.strips;
+    item += even;
+  }
+  const unsigned b = item / parts;
+  p.b = b;
+  p.seg = (int)(item - b * parts) + from;
   p.blk0 = p.seg * k.seg_blocks;
-  p.blk1 = p.blk0 + k.seg_blocks < k.blocks ? p.blk0 + k.seg_blocks : k.blocks;
+  p.blk1 = p.blk0 + k.seg_blocks < k.all ? p.blk0 + k.seg_blocks : k.all;
   return p;
 }
 
-// Step t of a strip of an array, as a base that is the same for the whole workgroup; a thread's own
-// part of the offset stays below 2^31 bytes (127 steps of at most GS_RECURRENCE_MAX_STRIDE fp32 elements,
-// 64 channels).
-__device__ __forceinline__ char* row(const Rows& r, int64_t b, int64_t t, int64_t strip_bytes) {
-  return r.p + b * r.batch + t * r.time + strip_bytes;
+// One block of a strip of an array as a buffer: its first byte and the strides are the same for the whole
+// workgroup (scalar registers), a thread adds one 32-bit offset, which stays below 2^31 (63 steps of at most
+// GS_RECURRENCE_MAX_STRIDE fp32 elements, 128 channels). Offset kNowhere is out of the buffer's range: a load
+// there gives zero and a store is dropped, so steps and channels that are not there need no branches.
+constexpr uint32_t kNowhere = 0x80000000u;
+// Cache policy of the rows' loads and stores: non-temporal.
+constexpr int kStream = 2;
+
+struct Block {
+  __amdgpu_buffer_rsrc_t at;
+  uint32_t time;
+  __device__ __forceinline__ Block(const Rows& r, int64_t b, int t0, int64_t strip_bytes)
+      : at(__builtin_amdgcn_make_buffer_rsrc(r.p + b * r.batch + t0 * r.time + strip_bytes, 0, kNowhere, 0x00027000)),
+        time((uint32_t)r.time) {}
+};
+
+template <int DT, int VEC, int AUX>
+__device__ __forceinline__ typename Pack<DT, VEC>::raw load(const Block& k, uint32_t off, uint32_t step) {
+  using raw = typename Pack<DT, VEC>::raw;
+  if constexpr (sizeof(raw) == 8)
+    return __builtin_bit_cast(raw, __builtin_amdgcn_raw_buffer_load_b64(k.at, off, step * k.time, AUX));
+  else if constexpr (sizeof(raw) == 4)
+    return __builtin_bit_cast(raw, __builtin_amdgcn_raw_buffer_load_b32(k.at, off, step * k.time, AUX));
+  else
+    return __builtin_bit_cast(raw, __builtin_amdgcn_raw_buffer_load_b16(k.at, off, step * k.time, AUX));
 }
 
-template <int DT, int VEC>
-__device__ __forceinline__ typename Pack<DT, VEC>::raw load(const char* base, uint32_t off) {
-  return *reinterpret_cast<const typename Pack<DT, VEC>::raw*>(base + off);
-}
-
-template <int DT, int VEC>
-__device__ __forceinline__ void store(char* base, uint32_t off, typename Pack<DT, VEC>::wide v) {
-  *reinterpret_cast<typename Pack<DT, VEC>::raw*>(base + off) = Pack<DT, VEC>::down(v);
+template <int DT, int VEC, int AUX>
+__device__ __forceinline__ void store(const Block& k, uint32_t off, uint32_t step, typename Pack<DT, VEC>::wide v) {
+  const auto raw = Pack<DT, VEC>::down(v);
+  if constexpr (sizeof raw == 8) {
+    typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u2, raw), k.at, off, step * k.time, AUX);
+  } else if constexpr (sizeof raw == 4) {
+    __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, raw), k.at, off, step * k.time, AUX);
+  } else {
+    __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, raw), k.at, off, step * k.time, AUX);
+  }
 }
 
 template <int VEC>
@@ -84,6 +124,21 @@ __device__ __forceinline__ void storef(float* p, typename Pack<GS_F32, VEC>::wid
   *reinterpret_cast<typename Pack<GS_F32, VEC>::wide*>(p) = v;
 }
 
+// Makes the compiler hold a value as it is from here on: it neither puts off what computes it nor keeps
+// what could be computed from it again (the fp32 form of 16-bit elements) beside it.
+template <typename T>
+__device__ __forceinline__ void pin(T& v) {
+  if constexpr (sizeof(T) == 8) {
+    uint64_t w = __builtin_bit_cast(uint64_t, v);
+    asm volatile("" : "+v"(w));
+    v = __builtin_bit_cast(T, w);
+  } else if constexpr (sizeof(T) == 4) {
+    uint32_t w = __builtin_bit_cast(uint32_t, v);
+    asm volatile("" : "+v"(w));
+    v = __builtin_bit_cast(T, w);
+  }
+}
+
 template <int VEC, typename V>
 __device__ __forceinline__ V join(V a, V h, V s) {  // a h + s, one rounding
   V r;
@@ -92,50 +147,50 @@ __device__ __forceinline__ V join(V a, V h, V s) {  // a h + s, one rounding
   return r;
 }
 
-// L steps of one array for one thread. Steps past the last token read the last token's row again
-// (the caller drops what they hold), so nothing beyond the sequence is touched.
+// L steps of one array for one thread, from step `first` of its block. FULL: the block ends before the
+// sequence does; otherwise the steps past `last` are not read and hold zero.
 template <int DT, int VEC, int L>
 struct Steps {
   typename Pack<DT, VEC>::raw v[L];
-  __device__ __forceinline__ void get(const Rows& r, int64_t b, int64_t t0, int64_t strip_bytes, int first,
-                                      uint32_t coff, int last) {
-    const char* base = row(r, b, t0, strip_bytes);
-    if (first + L - 1 <= last) {
-      const uint32_t off = (uint32_t)first * (uint32_t)r.time + coff;
+  template <bool FULL>
+  __device__ __forceinline__ void get(const Block& k, int first, uint32_t coff, int last, bool live) {
+    const uint32_t off = live ? (uint32_t)first * k.time + coff : kNowhere;
 #pragma unroll
-      for (int i = 0; i < L; ++i) v[i] = load<DT, VEC>(base + i * r.time, off);
-    } else {
-#pragma unroll
-      for (int i = 0; i < L; ++i) {
-        const int t = first + i < last ? first + i : last;
-        v[i] = load<DT, VEC>(base, (uint32_t)t * (uint32_t)r.time + coff);
-      }
-    }
+    for (int i = 0; i < L; ++i) v[i] = load<DT, VEC, kStream>(k, FULL || first + i <= last ? off : kNowhere, i);
   }
+  __device__ __forceinline__ typename Pack<DT, VEC>::wide at(int i) const { return Pack<DT, VEC>::up(v[i]); }
 };
 
+// Step i of a thread is padding.
+template <bool FULL>
+__device__ __forceinline__ bool padded(int first, int i, int last) {
+  return !FULL && first + i > last;
+}
+
 // The gates of L steps: kept a, taken 1 - a; padding keeps everything.
-template <int DT, int VEC, int L, typename V>
+template <bool FULL, int DT, int VEC, int L, typename V>
 __device__ __forceinline__ void gates(const Steps<DT, VEC, L>& f, int first, int last, V (&k)[L], V (&rest)[L]) {
 #pragma unroll
   for (int i = 0; i < L; ++i) {
-    const V z = Pack<DT, VEC>::up(f.v[i]);
+    const V z = f.at(i);
 #pragma unroll
     for (int j = 0; j < VEC; ++j) {
       float a, r;
       sigmoid_both(z[j], a, r);
-      k[i][j] = a;
-      rest[i][j] = r;
+      k[i][j] = padded<FULL>(first, i, last) ? 1.0f : a;
+      rest[i][j] = padded<FULL>(first, i, last) ? 0.0f : r;
     }
   }
-  if (first + L - 1 > last) {
+}
+
+template <int DT, int VEC, int L>
+__device__ __forceinline__ void zero_steps(const Rows& r, int64_t b, int t0, int64_t sb, int first, uint32_t coff,
+                                           bool live, int T) {
+  const Block k(r, b, t0, sb);
+  const uint32_t off = (uint32_t)first * k.time + coff;
 #pragma unroll
-    for (int i = 0; i < L; ++i)
-      if (first + i > last) {
-        k[i] = (V)1.0f;
-        rest[i] = (V)0.0f;
-      }
-  }
+  for (int i = 0; i < L; ++i)
+    store<DT, VEC, kStream>(k, live && t0 + first + i < T ? off : kNowhere, i, (typename Pack<DT, VEC>::wide)0.0f);
 }
 
 // work: for each sequence and segment, the map that its state before the segment joins last: [B][segs][2][C].
@@ -146,19 +201,19 @@ __device__ __forceinline__ float* slot_of(float* work, const Cut& k, int64_t b, 
 }
 
 template <int DT, int VEC, bool GATE, int W, int G, int L, bool REDUCE>
-__global__ void __launch_bounds__(W* G) k_recurrence_fwd(RecurrenceArgs a, Cut cut) {
+__global__ void __launch_bounds__(W* G, G > 1 ? 4 : 1) k_recurrence_fwd(RecurrenceArgs a, Cut cut) {
   using V = typename Pack<GS_F32, VEC>::wide;
   constexpr int kSpan = G * L;
-  __shared__ V maps[G > 1 ? 2 : 1][2][G > 1 ? G : 1][G > 1 ? W : 1];
-  const Place p = place_of(cut, 0);
+  __shared__ V maps[G > 1 ? 2 : 1][2][G][W];
+  const Place p = place_of<(G > 1)>(cut, cut.segs - (REDUCE ? 1 : 0), 0, a.B);
   if (p.b >= a.B) return;
   const int lane = threadIdx.x % W, g = threadIdx.x / W;
   const int64_t c0 = (int64_t)p.strip * (W * VEC);
   const bool live = c0 + lane * VEC < a.C;
-  const int64_t c = live ? c0 + lane * VEC : a.C - VEC;  // lanes past the last channel repeat it and store nothing
+  const int64_t c = live ? c0 + lane * VEC : a.C - VEC;  // for lanes past the last channel another one's state
   const int64_t sb = c0 * (int64_t)sizeof(typename Elem<DT>::type);
-  const uint32_t off = (uint32_t)(c - c0) * (uint32_t)sizeof(typename Elem<DT>::type);
-  const int64_t n = length_of(a, p.b);
+  const uint32_t off = (uint32_t)(lane * VEC) * (uint32_t)sizeof(typename Elem<DT>::type);
+  const int n = length_of(a, p.b), T = (int)a.T;
   V h = (V)0.0f, prod = (V)1.0f;
   if (REDUCE) {
     if (p.seg == 0 && live && g == 0) {
@@ -173,70 +228,85 @@ __global__ void __launch_bounds__(W* G) k_recurrence_fwd(RecurrenceArgs a, Cut c
   } else if (a.h0) {
     h = loadf<VEC>(a.h0 + p.b * a.C + c);
   }
-  for (int64_t blk = p.blk0; blk < p.blk1; ++blk) {
-    const int64_t t0 = blk * kSpan;
-    const int first = g * L;
-    if (t0 < n) {
-      const int last = n - t0 < kSpan ? (int)(n - t0) - 1 : kSpan - 1;
-      if (!REDUCE && a.states && g == 0 && live) storef<VEC>(a.states + (p.b * cut.blocks + blk) * a.C + c, h);
-      Steps<DT, VEC, L> xs, fs, os;
-      fs.get(a.f, p.b, t0, sb, first, off, last);
-      xs.get(a.x, p.b, t0, sb, first, off, last);
-      if (GATE && !REDUCE) os.get(a.o, p.b, t0, sb, first, off, last);
-      V k[L], in[L];
-      gates<DT, VEC, L>(fs, first, last, k, in);
-      V A = (V)1.0f, S = (V)0.0f;
+  const int first = g * L;
+  struct Loads {
+    Steps<DT, VEC, L> x, f, o;
+  };
+  auto fetch = [&](auto full, int blk, int last) {
+    constexpr bool FULL = decltype(full)::value;
+    const int t0 = blk * kSpan;
+    Loads m;
+    m.f.template get<FULL>(Block(a.f, p.b, t0, sb), first, off, last, live);
+    m.x.template get<FULL>(Block(a.x, p.b, t0, sb), first, off, last, live);
+    if (GATE && !REDUCE) m.o.template get<FULL>(Block(a.o, p.b, t0, sb), first, off, last, live);
+    return m;
+  };
+  auto block = [&](auto full, int blk, int last, const Loads& m) {
+    constexpr bool FULL = decltype(full)::value;
+    const int t0 = blk * kSpan;
+    V k[L], in[L];
+    gates<FULL>(m.f, first, last, k, in);
+    V A = (V)1.0f, S = (V)0.0f;
 #pragma unroll
-      for (int i = 0; i < L; ++i) {
-        V xi = Pack<DT, VEC>::up(xs.v[i]);
-        if (first + i > last) xi = (V)0.0f;  // padding may hold anything, NaN too
-        in[i] = in[i] * xi;
-        A = A * k[i];
-        S = join<VEC>(k[i], S, in[i]);
-      }
-      V mine = h;
-      if (G > 1) {
-        const int buf = (int)(blk & 1);
-        maps[buf][0][g][lane] = A;
-        maps[buf][1][g][lane] = S;
-        __syncthreads();
-#pragma unroll 4
-        for (int s = 0; s < G; ++s) {
-          if (s == g) mine = h;
-          const V As = maps[buf][0][s][lane];
-          h = join<VEC>(As, h, maps[buf][1][s][lane]);
-          if (REDUCE) prod = prod * As;
-        }
-      } else {
-        h = join<VEC>(A, h, S);
-        if (REDUCE) prod = prod * A;
-      }
-      if (!REDUCE) {
-        char* base = row(a.y, p.b, t0, sb);
+    for (int i = 0; i < L; ++i) {
+      in[i] = in[i] * m.x.at(i);
+      A = A * k[i];
+      S = join<VEC>(k[i], S, in[i]);
+    }
+    V mine = h;
+    if (G > 1) {
+      const int buf = blk & 1;
+      maps[buf][0][g][lane] = A;
+      maps[buf][1][g][lane] = S;
+      __syncthreads();
 #pragma unroll
-        for (int i = 0; i < L; ++i) {
-          mine = join<VEC>(k[i], mine, in[i]);
-          V out = mine;
-          if (GATE) {
-            const V z = Pack<DT, VEC>::up(os.v[i]);
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-              float s, r;
-              sigmoid_both(z[j], s, r);
-              out[j] = s * out[j];
-            }
-          }
-          if (first + i > last) out = (V)0.0f;
-          if (live && t0 + first + i < a.T)
-            store<DT, VEC>(base, (uint32_t)(first + i) * (uint32_t)a.y.time + off, out);
-        }
+      for (int s = 0; s < G; ++s) {
+        if (s == g) mine = h;
+        const V As = maps[buf][0][s][lane];
+        h = join<VEC>(As, h, maps[buf][1][s][lane]);
+        if (REDUCE) prod = prod * As;
       }
-    } else if (!REDUCE && live) {
-      char* base = row(a.y, p.b, t0, sb);
-      for (int i = 0; i < L && t0 + first + i < a.T; ++i)
-        store<DT, VEC>(base, (uint32_t)(first + i) * (uint32_t)a.y.time + off, (V)0.0f);
+    } else {
+      h = join<VEC>(A, h, S);
+      if (REDUCE) prod = prod * A;
+    }
+    if (REDUCE) return;
+    if (first % GS_RECURRENCE_BLOCK == 0 && a.states && live && (FULL || first <= last))
+      storef<VEC>(a.states + (p.b * cut.blocks + (t0 + first) / GS_RECURRENCE_BLOCK) * a.C + c, mine);
+    const Block to(a.y, p.b, t0, sb);
+    const uint32_t at = live ? (uint32_t)first * to.time + off : kNowhere;
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      mine = join<VEC>(k[i], mine, in[i]);
+      V out = mine;
+      if (GATE) {
+        const V z = m.o.at(i);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) out[j] = sigmoid_of(z[j]) * out[j];
+      }
+      if (padded<FULL>(first, i, last)) out = (V)0.0f;
+      store<DT, VEC, kStream>(to, FULL || t0 + first + i < T ? at : kNowhere, i, out);
+    }
+  };
+  // whole blocks, each one's loads under way while the one before is worked on; a last, part one; padding
+  const int whole = n / kSpan < p.blk1 ? n / kSpan : p.blk1;
+  int blk = p.blk0;
+  if (blk < whole) {
+    Loads now = fetch(std::true_type(), blk, kSpan - 1);
+    for (; blk < whole; ++blk) {
+      Loads next;
+      if (blk + 1 < whole) next = fetch(std::true_type(), blk + 1, kSpan - 1);
+      block(std::true_type(), blk, kSpan - 1, now);
+      now = next;
     }
   }
+  if (blk < p.blk1 && blk * kSpan < n) {
+    const int last = n - blk * kSpan - 1;
+    block(std::false_type(), blk, last, fetch(std::false_type(), blk, last));
+    ++blk;
+  }
+  if (!REDUCE)
+    for (; blk < p.blk1; ++blk) zero_steps<DT, VEC, L>(a.y, p.b, blk * kSpan, sb, first, off, live, T);
   if (g != 0 || !live) return;
   if (REDUCE) {
     float* m = slot_of(a.work, cut, p.b, p.seg + 1, a.C) + c;
@@ -248,19 +318,19 @@ __global__ void __launch_bounds__(W* G) k_recurrence_fwd(RecurrenceArgs a, Cut c
 }
 
 template <int DT, int VEC, bool GATE, int W, int G, int L, bool REDUCE>
-__global__ void __launch_bounds__(W* G) k_recurrence_bwd(RecurrenceArgs a, Cut cut) {
+__global__ void __launch_bounds__(W* G, G == 4 ? 3 : G == 8 ? 2 : 1) k_recurrence_bwd(RecurrenceArgs a, Cut cut) {
   using V = typename Pack<GS_F32, VEC>::wide;
   constexpr int kSpan = G * L;
-  __shared__ V maps[G > 1 ? 2 : 1][3][G > 1 ? G : 1][G > 1 ? W : 1];
-  const Place p = place_of(cut, REDUCE ? 1 : 0);
+  __shared__ V maps[G > 1 ? 2 : 1][3][G][W];
+  const Place p = place_of<(G > 1)>(cut, cut.segs - (REDUCE ? 1 : 0), REDUCE ? 1 : 0, a.B);
   if (p.b >= a.B) return;
   const int lane = threadIdx.x % W, g = threadIdx.x / W;
   const int64_t c0 = (int64_t)p.strip * (W * VEC);
   const bool live = c0 + lane * VEC < a.C;
   const int64_t c = live ? c0 + lane * VEC : a.C - VEC;
   const int64_t sb = c0 * (int64_t)sizeof(typename Elem<DT>::type);
-  const uint32_t off = (uint32_t)(c - c0) * (uint32_t)sizeof(typename Elem<DT>::type);
-  const int64_t n = length_of(a, p.b);
+  const uint32_t off = (uint32_t)(lane * VEC) * (uint32_t)sizeof(typename Elem<DT>::type);
+  const int n = length_of(a, p.b), T = (int)a.T;
   V carry = (V)0.0f, prod = (V)1.0f;
   if (REDUCE) {
     if (p.seg == cut.segs - 1 && live && g == 0) {
@@ -276,103 +346,132 @@ __global__ void __launch_bounds__(W* G) k_recurrence_bwd(RecurrenceArgs a, Cut c
   } else if (a.gh) {
     carry = loadf<VEC>(a.gh + p.b * a.C + c);
   }
-  for (int64_t blk = p.blk1 - 1; blk >= p.blk0; --blk) {
-    const int64_t t0 = blk * kSpan;
-    const int first = g * L;
-    if (t0 < n) {
-      const int last = n - t0 < kSpan ? (int)(n - t0) - 1 : kSpan - 1;
-      Steps<DT, VEC, L> xs, fs, os, gs;
-      fs.get(a.f, p.b, t0, sb, first, off, last);
-      gs.get(a.gy, p.b, t0, sb, first, off, last);
-      if (GATE) os.get(a.o, p.b, t0, sb, first, off, last);
-      V h = (V)0.0f;
-      if (!REDUCE) {
-        xs.get(a.x, p.b, t0, sb, first, off, last);
-        h = loadf<VEC>(a.states + (p.b * cut.blocks + blk) * a.C + c);
-      }
-      V k[L], rest[L], q[L], shut[L];  // shut: gy sigmoid(o) (1 - sigmoid(o)), the factor of h in do
-      gates<DT, VEC, L>(fs, first, last, k, rest);
-      V A = (V)1.0f, S = (V)0.0f, R = (V)0.0f;
+  const int first = g * L;
+  struct Loads {
+    Steps<DT, VEC, L> x, f, o, gy;
+    V h;
+  };
+  auto fetch = [&](auto full, int blk, int last) {
+    constexpr bool FULL = decltype(full)::value;
+    const int t0 = blk * kSpan;
+    Loads m;
+    m.f.template get<FULL>(Block(a.f, p.b, t0, sb), first, off, last, live);
+    m.gy.template get<FULL>(Block(a.gy, p.b, t0, sb), first, off, last, live);
+    if (GATE) m.o.template get<FULL>(Block(a.o, p.b, t0, sb), first, off, last, live);
+    if (!REDUCE) {
+      m.x.template get<FULL>(Block(a.x, p.b, t0, sb), first, off, last, live);
+      m.h = loadf<VEC>(a.states + (p.b * cut.blocks + t0 / GS_RECURRENCE_BLOCK) * a.C + c);
+    }
+    return m;
+  };
+  auto block = [&](auto full, int blk, int last, Loads& m) {
+    constexpr bool FULL = decltype(full)::value;
+    const int t0 = blk * kSpan;
+    V h = REDUCE ? (V)0.0f : m.h;
+    V k[L], rest[L], q[L], shut[L];  // shut: gy sigmoid(o) (1 - sigmoid(o)), the factor of h in do
+    gates<FULL>(m.f, first, last, k, rest);
+    V A = (V)1.0f, S = (V)0.0f, R = (V)0.0f;
 #pragma unroll
-      for (int i = 0; i < L; ++i) {
-        const bool pad = first + i > last;
-        q[i] = pad ? (V)0.0f : Pack<DT, VEC>::up(gs.v[i]);
-        if (GATE) {
-          const V z = Pack<DT, VEC>::up(os.v[i]);
+    for (int i = 0; i < L; ++i) {
+      q[i] = m.gy.at(i);
+      if (GATE) {
+        const V z = m.o.at(i);
 #pragma unroll
-          for (int j = 0; j < VEC; ++j) {
+        for (int j = 0; j < VEC; ++j) {
+          if (REDUCE) {
+            q[i][j] = q[i][j] * sigmoid_of(z[j]);
+          } else {
             float s, r;
-            sigmoid_both(pad ? 0.0f : z[j], s, r);
+            sigmoid_both(z[j], s, r);
             q[i][j] = q[i][j] * s;
             shut[i][j] = q[i][j] * r;
           }
         }
-        A = A * k[i];
-        if (!REDUCE) {
-          const V xi = pad ? (V)0.0f : Pack<DT, VEC>::up(xs.v[i]);
-          S = join<VEC>(k[i], S, rest[i] * xi);
-        }
       }
+      A = A * k[i];
+      if (!REDUCE) S = join<VEC>(k[i], S, rest[i] * m.x.at(i));
+    }
 #pragma unroll
-      for (int i = L - 1; i >= 0; --i) R = k[i] * (q[i] + R);
-      V c_in = carry;
-      if (G > 1) {
-        const int buf = (int)(blk & 1);
-        maps[buf][0][g][lane] = A;
-        maps[buf][1][g][lane] = R;
-        if (!REDUCE) maps[buf][2][g][lane] = S;
-        __syncthreads();
-#pragma unroll 4
-        for (int s = G - 1; s >= 0; --s) {
-          if (s == g) c_in = carry;
-          const V As = maps[buf][0][s][lane];
-          carry = join<VEC>(As, carry, maps[buf][1][s][lane]);
-          if (REDUCE) prod = prod * As;
-        }
-        if (!REDUCE) {
-          V hs = h;
-#pragma unroll 4
-          for (int s = 0; s < G - 1; ++s) {
-            hs = join<VEC>(maps[buf][0][s][lane], hs, maps[buf][2][s][lane]);
-            if (s == g - 1) h = hs;
-          }
-        }
-      } else {
-        carry = join<VEC>(A, carry, R);
-        if (REDUCE) prod = prod * A;
-      }
-      if (!REDUCE) {
-        V before[L];
+    for (int i = L - 1; i >= 0; --i) R = k[i] * (q[i] + R);
+    if (!REDUCE) {
 #pragma unroll
-        for (int i = 0; i < L; ++i) {
-          const V xi = first + i > last ? (V)0.0f : Pack<DT, VEC>::up(xs.v[i]);
-          before[i] = h;
-          h = join<VEC>(k[i], h, rest[i] * xi);
-          if (GATE) shut[i] = shut[i] * h;
-        }
+      for (int i = 0; i < L; ++i) {
+        pin(k[i]);
+        pin(rest[i]);
+        if (GATE) pin(shut[i]);
+      }
+    }
+    V c_in = carry;
+    if (G > 1) {
+      const int buf = blk & 1;
+      maps[buf][0][g][lane] = A;
+      maps[buf][1][g][lane] = R;
+      if (!REDUCE) maps[buf][2][g][lane] = S;
+      __syncthreads();
+      V hs = h;
 #pragma unroll
-        for (int i = L - 1; i >= 0; --i) {
-          const bool pad = first + i > last;
-          const V xi = pad ? (V)0.0f : Pack<DT, VEC>::up(xs.v[i]);
-          const V s = q[i] + c_in;
-          c_in = k[i] * s;
-          if (live && t0 + first + i < a.T) {
-            const uint32_t t = (uint32_t)(first + i);
-            // padding: rest = 0 and shut = 0
-            const V dx = rest[i] * s, df = s * (before[i] - xi) * (k[i] * rest[i]);
-            store<DT, VEC>(row(a.dx, p.b, t0, sb), t * (uint32_t)a.dx.time + off, dx);
-            store<DT, VEC>(row(a.df, p.b, t0, sb), t * (uint32_t)a.df.time + off, df);
-            if (GATE) store<DT, VEC>(row(a.dout, p.b, t0, sb), t * (uint32_t)a.dout.time + off, shut[i]);
-          }
+      for (int s = 0; s < G; ++s) {
+        const int r = G - 1 - s;
+        if (r == g) c_in = carry;
+        const V Ar = maps[buf][0][r][lane];
+        carry = join<VEC>(Ar, carry, maps[buf][1][r][lane]);
+        if (REDUCE) {
+          prod = prod * Ar;
+        } else {
+          if (s == g) h = hs;
+          hs = join<VEC>(maps[buf][0][s][lane], hs, maps[buf][2][s][lane]);
         }
       }
-    } else if (!REDUCE && live) {
-      for (int i = 0; i < L && t0 + first + i < a.T; ++i) {
-        const uint32_t t = (uint32_t)(first + i);
-        store<DT, VEC>(row(a.dx, p.b, t0, sb), t * (uint32_t)a.dx.time + off, (V)0.0f);
-        store<DT, VEC>(row(a.df, p.b, t0, sb), t * (uint32_t)a.df.time + off, (V)0.0f);
-        if (GATE) store<DT, VEC>(row(a.dout, p.b, t0, sb), t * (uint32_t)a.dout.time + off, (V)0.0f);
-      }
+    } else {
+      carry = join<VEC>(A, carry, R);
+      if (REDUCE) prod = prod * A;
+    }
+    if (REDUCE) return;
+#pragma unroll
+    for (int i = 0; i < L; ++i) pin(m.x.v[i]);
+#pragma unroll
+    for (int i = L - 1; i >= 0; --i) {  // q becomes s
+      q[i] = q[i] + c_in;
+      c_in = k[i] * q[i];
+    }
+    const Block to_x(a.dx, p.b, t0, sb), to_f(a.df, p.b, t0, sb), to_o(a.dout, p.b, t0, sb);
+    const uint32_t at_x = live ? (uint32_t)first * to_x.time + off : kNowhere;
+    const uint32_t at_f = live ? (uint32_t)first * to_f.time + off : kNowhere;
+    const uint32_t at_o = live ? (uint32_t)first * to_o.time + off : kNowhere;
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      const V xi = m.x.at(i);
+      const V dx = rest[i] * q[i], df = (dx * k[i]) * (h - xi);  // padding: rest and shut are 0
+      h = join<VEC>(k[i], h, rest[i] * xi);
+      const bool in = FULL || t0 + first + i < T;
+      store<DT, VEC, kStream>(to_x, in ? at_x : kNowhere, i, dx);
+      store<DT, VEC, kStream>(to_f, in ? at_f : kNowhere, i, df);
+      if (GATE) store<DT, VEC, kStream>(to_o, in ? at_o : kNowhere, i, shut[i] * h);
+    }
+  };
+  int blk = p.blk1 - 1;
+  if (!REDUCE) {
+    for (; blk >= p.blk0 && blk * kSpan >= n; --blk) {
+      zero_steps<DT, VEC, L>(a.dx, p.b, blk * kSpan, sb, first, off, live, T);
+      zero_steps<DT, VEC, L>(a.df, p.b, blk * kSpan, sb, first, off, live, T);
+      if (GATE) zero_steps<DT, VEC, L>(a.dout, p.b, blk * kSpan, sb, first, off, live, T);
+    }
+  } else if (blk * kSpan >= n) {
+    blk = (n + kSpan - 1) / kSpan - 1;
+  }
+  if (blk >= p.blk0 && (blk + 1) * kSpan > n) {
+    const int last = n - blk * kSpan - 1;
+    Loads m = fetch(std::false_type(), blk, last);
+    block(std::false_type(), blk, last, m);
+    --blk;
+  }
+  if (blk >= p.blk0) {
+    Loads now = fetch(std::true_type(), blk, kSpan - 1);
+    for (; blk >= p.blk0; --blk) {
+      Loads next;
+      if (blk > p.blk0) next = fetch(std::true_type(), blk - 1, kSpan - 1);
+      block(std::true_type(), blk, kSpan - 1, now);
+      now = next;
     }
   }
   if (g != 0 || !live) return;
@@ -385,49 +484,63 @@ __global__ void __launch_bounds__(W* G) k_recurrence_bwd(RecurrenceArgs a, Cut c
   }
 }
 
-// Steps of one thread, threads across the channels, groups along time: single tokens, up to eight
-// steps, anything longer.
+constexpr int kSteps = 8;           // of a thread
+constexpr int kChip = 256;          // workgroups that give every CU one
+constexpr int kMaxSegs = 128;
+
+// How a direction is cut. Single tokens and up to eight steps need no groups. More steps take eight groups a
+// workgroup; the backward pass, which needs 1.7 times the registers, takes four where that still gives the
+// CUs more than one workgroup (32 x 512 x 1,500 bf16, 384 workgroups: 106 us with four groups, 128 with eight;
+// 16 x 4,096 x 2,048, 256 workgroups: 490 and 412). At most half a workgroup a CU is split along time to two a CU,
+// which costs reading two or three arrays twice.
+Cut cut_of(int64_t B, int64_t T, int64_t C, int vec, bool backward) {
+  Cut k{};
+  const int64_t across = 64 * vec;
+  k.strips = (unsigned)((C + across - 1) / across);
+  k.blocks = (int)GS_RECURRENCE_BLOCKS(T);
+  k.segs = 1;
+  const int64_t have = B * (int64_t)k.strips;
+  const bool split = 2 * have <= kChip;
+  k.groups = T <= kSteps ? 1 : backward && (split || 4 * have > 5 * kChip) ? 4 : 8;
+  const int64_t span = T <= 1 ? 1 : k.groups * kSteps;
+  k.all = (int)((T + span - 1) / span);
+  k.seg_blocks = k.all;
+  if (split && k.all > 1) {
+    int64_t segs = 2 * kChip / have;
+    segs = segs < k.all ? segs : k.all;
+    segs = segs < kMaxSegs ? segs : kMaxSegs;
+    k.seg_blocks = (int)((k.all + segs - 1) / segs);
+    k.segs = (k.all + k.seg_blocks - 1) / k.seg_blocks;
+  }
+  return k;
+}
+
 template <int DT, int VEC, bool GATE, bool REDUCE>
 void forward(hipStream_t s, const RecurrenceArgs& a, const Cut& k, dim3 grid) {
   if (a.T <= 1)
     k_recurrence_fwd<DT, VEC, GATE, 64, 1, 1, false><<<grid, 64, 0, s>>>(a, k);
-  else if (a.T <= 8)
-    k_recurrence_fwd<DT, VEC, GATE, 64, 1, 8, false><<<grid, 64, 0, s>>>(a, k);
+  else if (k.groups == 1)
+    k_recurrence_fwd<DT, VEC, GATE, 64, 1, kSteps, false><<<grid, 64, 0, s>>>(a, k);
   else
-    k_recurrence_fwd<DT, VEC, GATE, 32, 16, 8, REDUCE><<<grid, 512, 0, s>>>(a, k);
+    k_recurrence_fwd<DT, VEC, GATE, 64, 8, kSteps, REDUCE><<<grid, 512, 0, s>>>(a, k);
 }
 
 template <int DT, int VEC, bool GATE, bool REDUCE>
 void backward(hipStream_t s, const RecurrenceArgs& a, const Cut& k, dim3 grid) {
   if (a.T <= 1)
     k_recurrence_bwd<DT, VEC, GATE, 64, 1, 1, false><<<grid, 64, 0, s>>>(a, k);
-  else if (a.T <= 8)
-    k_recurrence_bwd<DT, VEC, GATE, 64, 1, 8, false><<<grid, 64, 0, s>>>(a, k);
-  else
-    k_recurrence_bwd<DT, VEC, GATE, 32, 16, 8, REDUCE><<<grid, 512, 0, s>>>(a, k);
+  else if (k.groups == 1)
+    k_recurrence_bwd<DT, VEC, GATE, 64, 1, kSteps, false><<<grid, 64, 0, s>>>(a, k);
+  else if (k.groups == 4)
+    k_recurrence_bwd<DT, VEC, GATE, 64, 4, kSteps, REDUCE><<<grid, 256, 0, s>>>(a, k);
+  else if (!REDUCE)
+    k_recurrence_bwd<DT, VEC, GATE, 64, 8, kSteps, false><<<grid, 512, 0, s>>>(a, k);
 }
 
-Cut cut_of(int64_t B, int64_t T, int64_t C, int vec) {
-  Cut k{};
-  const int64_t across = (T > 8 ? 32 : 64) * vec;
-  k.strips = (unsigned)((C + across - 1) / across);
-  k.blocks = T > 8 ? GS_RECURRENCE_BLOCKS(T) : T > 0 ? 1 : 0;
-  k.segs = 1;
-  k.seg_blocks = k.blocks;
-  const int64_t groups = B * (int64_t)k.strips;
-  if (2 * groups <= kWantGroups && k.blocks > 1) {
-    int64_t segs = kWantGroups / groups;
-    segs = segs < k.blocks ? segs : k.blocks;
-    segs = segs < kMaxSegs ? segs : kMaxSegs;
-    k.seg_blocks = (k.blocks + segs - 1) / segs;
-    k.segs = (int)((k.blocks + k.seg_blocks - 1) / k.seg_blocks);
-  }
-  return k;
-}
-
+// strips x parts x B is below 2^31: the [B][C] states of that many workgroups do not fit any memory.
 dim3 grid_of(const Cut& k, int parts, int64_t B) {
-  const int64_t y = B < kGridY ? B : kGridY;
-  return dim3(k.strips * (unsigned)parts, (unsigned)y, (unsigned)((B + y - 1) / y));
+  const int64_t n = (int64_t)k.strips * parts * B;
+  return dim3((unsigned)(n < kGridX ? n : kGridX), (unsigned)((n + kGridX - 1) / kGridX));
 }
 
 // Two channels a lane where every row of every array starts on a pair of elements.
@@ -460,8 +573,9 @@ void with_type(int dtype, bool two, bool gate, F f) {
 // For each sequence and segment one map; more segments where a lane takes two channels.
 int64_t recurrence_work(int64_t B, int64_t T, int64_t C, int) {
   if (B == 0 || T == 0 || C == 0) return 0;
-  const Cut k = cut_of(B, T, C, C % 2 == 0 ? 2 : 1);
-  return k.segs > 1 ? B * k.segs * 2 * C * (int64_t)sizeof(float) : 0;
+  const int vec = C % 2 == 0 ? 2 : 1;
+  const int f = cut_of(B, T, C, vec, false).segs, b = cut_of(B, T, C, vec, true).segs, segs = f > b ? f : b;
+  return segs > 1 ? B * segs * 2 * C * (int64_t)sizeof(float) : 0;
 }
 
 hipError_t launch_recurrence_forward(hipStream_t s, int dtype, const RecurrenceArgs& a) {
@@ -469,7 +583,7 @@ hipError_t launch_recurrence_forward(hipStream_t s, int dtype, const RecurrenceA
   const bool two = a.C % 2 == 0 && (a.T == 0 || (pairs(a.x, bytes) && pairs(a.f, bytes) && pairs(a.y, bytes) &&
                                                  (!a.o.p || pairs(a.o, bytes)))) &&
                    pairs(a.h0) && pairs(a.h_last) && pairs(a.states) && pairs(a.work);
-  const Cut k = cut_of(a.B, a.T, a.C, two ? 2 : 1);
+  const Cut k = cut_of(a.B, a.T, a.C, two ? 2 : 1, false);
   with_type(dtype, two, a.o.p != nullptr, [&](auto dt, auto vec, auto gate) {
     constexpr int DT = decltype(dt)::value, VEC = decltype(vec)::value;
     constexpr bool GATE = decltype(gate)::value;
@@ -485,7 +599,7 @@ hipError_t launch_recurrence_backward(hipStream_t s, int dtype, const Recurrence
                    (a.T == 0 || (pairs(a.x, bytes) && pairs(a.f, bytes) && pairs(a.gy, bytes) && pairs(a.dx, bytes) &&
                                  pairs(a.df, bytes) && (!a.o.p || (pairs(a.o, bytes) && pairs(a.dout, bytes))))) &&
                    pairs(a.gh) && pairs(a.dh0) && pairs(a.states) && pairs(a.work);
-  const Cut k = cut_of(a.B, a.T, a.C, two ? 2 : 1);
+  const Cut k = cut_of(a.B, a.T, a.C, two ? 2 : 1, true);
   with_type(dtype, two, a.o.p != nullptr, [&](auto dt, auto vec, auto gate) {
     constexpr int DT = decltype(dt)::value, VEC = decltype(vec)::value;
     constexpr bool GATE = decltype(gate)::value;

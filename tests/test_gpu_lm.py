@@ -57,8 +57,8 @@ def run_and_check(i, lengths=None, what=""):
     return got
 
 
-# one token, the edges of a block of saved states (128), several blocks, an odd number of them
-@pytest.mark.parametrize("T", [1, 2, 7, 8, 9, 16, 17, 127, 128, 129, 300, 1000])
+# one token, the edges of a block of saved states (64), several blocks, an odd number of them
+@pytest.mark.parametrize("T", [1, 2, 7, 8, 9, 16, 17, 63, 64, 65, 127, 128, 129, 300, 1000])
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
 def test_recurrence_lengths_of_time(T, dtype):
     run_and_check(inputs(T, 2, T, 40, dtype), what=f"T={T}")
