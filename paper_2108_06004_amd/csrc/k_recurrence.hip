@@ -79,8 +79,12 @@ __device__ __forceinline__ Place place_of(const Cut& k, unsigned parts, int from
 // GS_RECURRENCE_MAX_STRIDE fp32 elements, 128 channels). Offset kNowhere is out of the buffer's range: a load
 // there gives zero and a store is dropped, so steps and channels that are not there need no branches.
 constexpr uint32_t kNowhere = 0x80000000u;
-// Cache policy of the rows' loads and stores: non-temporal.
-constexpr int kStream = 2;
+// Cache policies: through the caches, or past them (non-temporal). Rows that start and end on 128-byte lines are read
+// and reduced past the caches (16 x 4,096 x 2,048 bf16 forward 243 us through them, 220 past; reducing 1 x 65,536 x
+// 1,024 75 and 49), rows that share lines with their neighbours through them (64 x 512 x 1,500: 89 and 95). y is
+// stored past them (64 x 512 x 1,500: 106 us through them, 89 past), gradients through them (219 us past, 146
+// through).
+constexpr int kCached = 0, kPast = 2;
 
 struct Block {
   __amdgpu_buffer_rsrc_t at;
@@ -149,14 +153,14 @@ __device__ __forceinline__ V join(V a, V h, V s) {  // a h + s, one rounding
 
 // L steps of one array for one thread, from step `first` of its block. FULL: the block ends before the
 // sequence does; otherwise the steps past `last` are not read and hold zero.
-template <int DT, int VEC, int L>
+template <int DT, int VEC, int L, int AUX>
 struct Steps {
   typename Pack<DT, VEC>::raw v[L];
   template <bool FULL>
   __device__ __forceinline__ void get(const Block& k, int first, uint32_t coff, int last, bool live) {
     const uint32_t off = live ? (uint32_t)first * k.time + coff : kNowhere;
 #pragma unroll
-    for (int i = 0; i < L; ++i) v[i] = load<DT, VEC, kStream>(k, FULL || first + i <= last ? off : kNowhere, i);
+    for (int i = 0; i < L; ++i) v[i] = load<DT, VEC, AUX>(k, FULL || first + i <= last ? off : kNowhere, i);
   }
   __device__ __forceinline__ typename Pack<DT, VEC>::wide at(int i) const { return Pack<DT, VEC>::up(v[i]); }
 };
@@ -168,8 +172,8 @@ __device__ __forceinline__ bool padded(int first, int i, int last) {
 }
 
 // The gates of L steps: kept a, taken 1 - a; padding keeps everything.
-template <bool FULL, int DT, int VEC, int L, typename V>
-__device__ __forceinline__ void gates(const Steps<DT, VEC, L>& f, int first, int last, V (&k)[L], V (&rest)[L]) {
+template <bool FULL, int DT, int VEC, int L, int AUX, typename V>
+__device__ __forceinline__ void gates(const Steps<DT, VEC, L, AUX>& f, int first, int last, V (&k)[L], V (&rest)[L]) {
 #pragma unroll
   for (int i = 0; i < L; ++i) {
     const V z = f.at(i);
@@ -190,7 +194,7 @@ __device__ __forceinline__ void zero_steps(const Rows& r, int64_t b, int t0, int
   const uint32_t off = (uint32_t)first * k.time + coff;
 #pragma unroll
   for (int i = 0; i < L; ++i)
-    store<DT, VEC, kStream>(k, live && t0 + first + i < T ? off : kNowhere, i, (typename Pack<DT, VEC>::wide)0.0f);
+    store<DT, VEC, kCached>(k, live && t0 + first + i < T ? off : kNowhere, i, (typename Pack<DT, VEC>::wide)0.0f);
 }
 
 // work: for each sequence and segment, the map that its state before the segment joins last: [B][segs][2][C].
@@ -200,7 +204,7 @@ __device__ __forceinline__ float* slot_of(float* work, const Cut& k, int64_t b, 
   return work + ((b * k.segs + s) * 2) * C;
 }
 
-template <int DT, int VEC, bool GATE, int W, int G, int L, bool REDUCE>
+template <int DT, int VEC, bool GATE, int W, int G, int L, bool REDUCE, int AUX>
 __global__ void __launch_bounds__(W* G, G > 1 ? 4 : 1) k_recurrence_fwd(RecurrenceArgs a, Cut cut) {
   using V = typename Pack<GS_F32, VEC>::wide;
   constexpr int kSpan = G * L;
@@ -230,7 +234,7 @@ __global__ void __launch_bounds__(W* G, G > 1 ? 4 : 1) k_recurrence_fwd(Recurren
   }
   const int first = g * L;
   struct Loads {
-    Steps<DT, VEC, L> x, f, o;
+    Steps<DT, VEC, L, AUX> x, f, o;
   };
   auto fetch = [&](auto full, int blk, int last) {
     constexpr bool FULL = decltype(full)::value;
@@ -285,7 +289,7 @@ __global__ void __launch_bounds__(W* G, G > 1 ? 4 : 1) k_recurrence_fwd(Recurren
         for (int j = 0; j < VEC; ++j) out[j] = sigmoid_of(z[j]) * out[j];
       }
       if (padded<FULL>(first, i, last)) out = (V)0.0f;
-      store<DT, VEC, kStream>(to, FULL || t0 + first + i < T ? at : kNowhere, i, out);
+      store<DT, VEC, kPast>(to, FULL || t0 + first + i < T ? at : kNowhere, i, out);
     }
   };
   // whole blocks, each one's loads under way while the one before is worked on; a last, part one; padding
@@ -317,7 +321,7 @@ __global__ void __launch_bounds__(W* G, G > 1 ? 4 : 1) k_recurrence_fwd(Recurren
   }
 }
 
-template <int DT, int VEC, bool GATE, int W, int G, int L, bool REDUCE>
+template <int DT, int VEC, bool GATE, int W, int G, int L, bool REDUCE, int AUX>
 __global__ void __launch_bounds__(W* G, G == 4 ? 3 : G == 8 ? 2 : 1) k_recurrence_bwd(RecurrenceArgs a, Cut cut) {
   using V = typename Pack<GS_F32, VEC>::wide;
   constexpr int kSpan = G * L;
@@ -348,7 +352,7 @@ __global__ void __launch_bounds__(W* G, G == 4 ? 3 : G == 8 ? 2 : 1) k_recurrenc
   }
   const int first = g * L;
   struct Loads {
-    Steps<DT, VEC, L> x, f, o, gy;
+    Steps<DT, VEC, L, AUX> x, f, o, gy;
     V h;
   };
   auto fetch = [&](auto full, int blk, int last) {
@@ -444,9 +448,9 @@ __global__ void __launch_bounds__(W* G, G == 4 ? 3 : G == 8 ? 2 : 1) k_recurrenc
       const V dx = rest[i] * q[i], df = (dx * k[i]) * (h - xi);  // padding: rest and shut are 0
       h = join<VEC>(k[i], h, rest[i] * xi);
       const bool in = FULL || t0 + first + i < T;
-      store<DT, VEC, kStream>(to_x, in ? at_x : kNowhere, i, dx);
-      store<DT, VEC, kStream>(to_f, in ? at_f : kNowhere, i, df);
-      if (GATE) store<DT, VEC, kStream>(to_o, in ? at_o : kNowhere, i, shut[i] * h);
+      store<DT, VEC, kCached>(to_x, in ? at_x : kNowhere, i, dx);
+      store<DT, VEC, kCached>(to_f, in ? at_f : kNowhere, i, df);
+      if (GATE) store<DT, VEC, kCached>(to_o, in ? at_o : kNowhere, i, shut[i] * h);
     }
   };
   int blk = p.blk1 - 1;
@@ -490,17 +494,16 @@ constexpr int kMaxSegs = 128;
 
 // How a direction is cut. Single tokens and up to eight steps need no groups. More steps take eight groups a
 // workgroup; the backward pass, which needs 1.7 times the registers, takes four where that still gives the
-// CUs more than one workgroup (32 x 512 x 1,500 bf16, 384 workgroups: 106 us with four groups, 128 with eight;
-// 16 x 4,096 x 2,048, 256 workgroups: 490 and 412). At most half a workgroup a CU is split along time to two a CU,
-// which costs reading two or three arrays twice.
+// CUs more than one workgroup each (16 x 4,096 x 2,048 bf16, 256 workgroups: 490 us with four groups, 412 with
+// eight). At most half a workgroup a CU: time is split to two a CU, which costs reading two or three arrays twice
+// (1 x 65,536 x 1,024: 256 workgroups 178 us forward, 512 160, 1,024 175).
 Cut cut_of(int64_t B, int64_t T, int64_t C, int vec, bool backward) {
   Cut k{};
-  const int64_t across = 64 * vec;
-  k.strips = (unsigned)((C + across - 1) / across);
+  k.strips = (unsigned)((C + 64 * vec - 1) / (64 * vec));
   k.blocks = (int)GS_RECURRENCE_BLOCKS(T);
   k.segs = 1;
   const int64_t have = B * (int64_t)k.strips;
-  const bool split = 2 * have <= kChip;
+  const bool split = T > kSteps && 2 * have <= kChip;
   k.groups = T <= kSteps ? 1 : backward && (split || 4 * have > 5 * kChip) ? 4 : 8;
   const int64_t span = T <= 1 ? 1 : k.groups * kSteps;
   k.all = (int)((T + span - 1) / span);
@@ -516,25 +519,29 @@ Cut cut_of(int64_t B, int64_t T, int64_t C, int vec, bool backward) {
 }
 
 template <int DT, int VEC, bool GATE, bool REDUCE>
-void forward(hipStream_t s, const RecurrenceArgs& a, const Cut& k, dim3 grid) {
+void forward(hipStream_t s, const RecurrenceArgs& a, const Cut& k, dim3 grid, bool lines) {
   if (a.T <= 1)
-    k_recurrence_fwd<DT, VEC, GATE, 64, 1, 1, false><<<grid, 64, 0, s>>>(a, k);
+    k_recurrence_fwd<DT, VEC, GATE, 64, 1, 1, false, kCached><<<grid, 64, 0, s>>>(a, k);
   else if (k.groups == 1)
-    k_recurrence_fwd<DT, VEC, GATE, 64, 1, kSteps, false><<<grid, 64, 0, s>>>(a, k);
+    k_recurrence_fwd<DT, VEC, GATE, 64, 1, kSteps, false, kCached><<<grid, 64, 0, s>>>(a, k);
+  else if (lines)
+    k_recurrence_fwd<DT, VEC, GATE, 64, 8, kSteps, REDUCE, kPast><<<grid, 512, 0, s>>>(a, k);
   else
-    k_recurrence_fwd<DT, VEC, GATE, 64, 8, kSteps, REDUCE><<<grid, 512, 0, s>>>(a, k);
+    k_recurrence_fwd<DT, VEC, GATE, 64, 8, kSteps, REDUCE, kCached><<<grid, 512, 0, s>>>(a, k);
 }
 
 template <int DT, int VEC, bool GATE, bool REDUCE>
-void backward(hipStream_t s, const RecurrenceArgs& a, const Cut& k, dim3 grid) {
+void backward(hipStream_t s, const RecurrenceArgs& a, const Cut& k, dim3 grid, bool lines) {
   if (a.T <= 1)
-    k_recurrence_bwd<DT, VEC, GATE, 64, 1, 1, false><<<grid, 64, 0, s>>>(a, k);
+    k_recurrence_bwd<DT, VEC, GATE, 64, 1, 1, false, kCached><<<grid, 64, 0, s>>>(a, k);
   else if (k.groups == 1)
-    k_recurrence_bwd<DT, VEC, GATE, 64, 1, kSteps, false><<<grid, 64, 0, s>>>(a, k);
-  else if (k.groups == 4)
-    k_recurrence_bwd<DT, VEC, GATE, 64, 4, kSteps, REDUCE><<<grid, 256, 0, s>>>(a, k);
-  else if (!REDUCE)
-    k_recurrence_bwd<DT, VEC, GATE, 64, 8, kSteps, false><<<grid, 512, 0, s>>>(a, k);
+    k_recurrence_bwd<DT, VEC, GATE, 64, 1, kSteps, false, kCached><<<grid, 64, 0, s>>>(a, k);
+  else if (k.groups == 8)
+    k_recurrence_bwd<DT, VEC, GATE, 64, 8, kSteps, false, kCached><<<grid, 512, 0, s>>>(a, k);
+  else if (REDUCE && lines)
+    k_recurrence_bwd<DT, VEC, GATE, 64, 4, kSteps, REDUCE, REDUCE ? kPast : kCached><<<grid, 256, 0, s>>>(a, k);
+  else
+    k_recurrence_bwd<DT, VEC, GATE, 64, 4, kSteps, REDUCE, kCached><<<grid, 256, 0, s>>>(a, k);
 }
 
 // strips x parts x B is below 2^31: the [B][C] states of that many workgroups do not fit any memory.
@@ -549,19 +556,21 @@ bool pairs(const Rows& r, int bytes) {
   return ((uintptr_t)r.p & m) == 0 && (r.batch & m) == 0 && (r.time & m) == 0;
 }
 
+// Every row of every step starts on a 128-byte line.
+bool lines(const Rows& r) { return (((uintptr_t)r.p | r.batch | r.time) & 127) == 0; }
+
 bool pairs(const float* p) { return ((uintptr_t)p & 7) == 0; }
 
+// Calls f with the element type, the channels of a lane and whether there is an output gate as constants.
 template <typename F>
 void with_type(int dtype, bool two, bool gate, F f) {
   auto g = [&](auto dt) {
-    constexpr int DT = decltype(dt)::value;
-    using True = std::true_type;
-    using False = std::false_type;
+    using One = std::integral_constant<int, 1>;
+    using Two = std::integral_constant<int, 2>;
     if (two)
-      gate ? f(dt, std::integral_constant<int, 2>(), True()) : f(dt, std::integral_constant<int, 2>(), False());
+      gate ? f(dt, Two(), std::true_type()) : f(dt, Two(), std::false_type());
     else
-      gate ? f(dt, std::integral_constant<int, 1>(), True()) : f(dt, std::integral_constant<int, 1>(), False());
-    (void)DT;
+      gate ? f(dt, One(), std::true_type()) : f(dt, One(), std::false_type());
   };
   if (dtype == GS_F32) g(std::integral_constant<int, GS_F32>());
   if (dtype == GS_BF16) g(std::integral_constant<int, GS_BF16>());
@@ -584,11 +593,12 @@ hipError_t launch_recurrence_forward(hipStream_t s, int dtype, const RecurrenceA
                                                  (!a.o.p || pairs(a.o, bytes)))) &&
                    pairs(a.h0) && pairs(a.h_last) && pairs(a.states) && pairs(a.work);
   const Cut k = cut_of(a.B, a.T, a.C, two ? 2 : 1, false);
+  const bool whole = lines(a.x) && lines(a.f) && lines(a.o);
   with_type(dtype, two, a.o.p != nullptr, [&](auto dt, auto vec, auto gate) {
     constexpr int DT = decltype(dt)::value, VEC = decltype(vec)::value;
     constexpr bool GATE = decltype(gate)::value;
-    if (k.segs > 1) forward<DT, VEC, false, true>(s, a, k, grid_of(k, k.segs - 1, a.B));
-    forward<DT, VEC, GATE, false>(s, a, k, grid_of(k, k.segs, a.B));
+    if (k.segs > 1) forward<DT, VEC, false, true>(s, a, k, grid_of(k, k.segs - 1, a.B), whole);
+    forward<DT, VEC, GATE, false>(s, a, k, grid_of(k, k.segs, a.B), whole);
   });
   return hipGetLastError();
 }
@@ -600,11 +610,12 @@ hipError_t launch_recurrence_backward(hipStream_t s, int dtype, const Recurrence
                                  pairs(a.df, bytes) && (!a.o.p || (pairs(a.o, bytes) && pairs(a.dout, bytes))))) &&
                    pairs(a.gh) && pairs(a.dh0) && pairs(a.states) && pairs(a.work);
   const Cut k = cut_of(a.B, a.T, a.C, two ? 2 : 1, true);
+  const bool whole = lines(a.gy) && lines(a.f) && lines(a.o);
   with_type(dtype, two, a.o.p != nullptr, [&](auto dt, auto vec, auto gate) {
     constexpr int DT = decltype(dt)::value, VEC = decltype(vec)::value;
     constexpr bool GATE = decltype(gate)::value;
-    if (k.segs > 1) backward<DT, VEC, GATE, true>(s, a, k, grid_of(k, k.segs - 1, a.B));
-    backward<DT, VEC, GATE, false>(s, a, k, grid_of(k, k.segs, a.B));
+    if (k.segs > 1) backward<DT, VEC, GATE, true>(s, a, k, grid_of(k, k.segs - 1, a.B), whole);
+    backward<DT, VEC, GATE, false>(s, a, k, grid_of(k, k.segs, a.B), whole);
   });
   return hipGetLastError();
 }
