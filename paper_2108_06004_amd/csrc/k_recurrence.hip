@@ -496,7 +496,8 @@ constexpr int kMaxSegs = 128;
 // workgroup; the backward pass, which needs 1.7 times the registers, takes four where that still gives the
 // CUs more than one workgroup each (16 x 4,096 x 2,048 bf16, 256 workgroups: 490 us with four groups, 412 with
 // eight). At most half a workgroup a CU: time is split to two a CU, which costs reading two or three arrays twice
-// (1 x 65,536 x 1,024: 256 workgroups 178 us forward, 512 160, 1,024 175).
+// (1 x 65,536 x 1,024: 256 workgroups 178 us forward, 512 160, 1,024 175), to four where a segment would be
+// shorter than eight blocks (5 x 1,037 x 1,500 fp16: 34 us with two a CU, 27 with four).
 Cut cut_of(int64_t B, int64_t T, int64_t C, int vec, bool backward) {
   Cut k{};
   k.strips = (unsigned)((C + 64 * vec - 1) / (64 * vec));
@@ -510,6 +511,7 @@ Cut cut_of(int64_t B, int64_t T, int64_t C, int vec, bool backward) {
   k.seg_blocks = k.all;
   if (split && k.all > 1) {
     int64_t segs = 2 * kChip / have;
+    if (k.all < 8 * segs) segs *= 2;
     segs = segs < k.all ? segs : k.all;
     segs = segs < kMaxSegs ? segs : kMaxSegs;
     k.seg_blocks = (int)((k.all + segs - 1) / segs);
