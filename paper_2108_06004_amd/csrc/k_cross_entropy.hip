@@ -16,16 +16,32 @@ namespace {
 constexpr int kTail = 256;  // threads that count rows and sum losses
 constexpr int kInlineCount = 256;  // rows that every workgroup counts by itself
 constexpr int kPartThreads = 256;
-constexpr int kPartVecs = 8;          // 16-byte pieces a thread takes of a part, at least
-constexpr int kMaxParts = 256;
+constexpr int kPartVecs = 4;          // 16-byte pieces a thread takes of a part, at least
+constexpr int kMaxParts = kPartThreads;
 constexpr int kRowThreads = 1024;
 constexpr int kRowPieces = 16;  // longest row in registers: 16 pieces of 1,024 threads, 256 KB
-constexpr int kSplitWant = 256;  // workgroups that few long rows are split into
+constexpr int kSplitWant = 2048;  // workgroups that rows are split into
+constexpr int kFewRows = 64, kLongRow = 8192;  // rows this few of pieces this many are split although registers hold them
 
 __device__ __forceinline__ float inf() { return __builtin_inff(); }
 
 // e^d for d <= 0 (and NaN).
 __device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
+
+// (maximum, sum of e^(z - maximum)) of what has been seen; a maximum of -inf stands for 0 in the sum.
+struct Seen {
+  float top, sum;
+};
+
+__device__ __forceinline__ float base_of(float top) { return top == -inf() ? 0.0f : top; }
+
+// A side that has seen nothing (or only -inf, or NaN) keeps its sum, 0 or NaN, as it is.
+__device__ __forceinline__ float moved(Seen p, float top) { return p.top == -inf() ? p.sum : p.sum * exp_of(p.top - top); }
+
+__device__ __forceinline__ Seen join(Seen p, Seen q) {
+  const float top = fmaxf(p.top, q.top);
+  return Seen{top, moved(p, top) + moved(q, top)};
+}
 
 // The sum of the losses and the rows that count.
 struct Tally {
@@ -35,6 +51,7 @@ struct Tally {
 
 // A value of the lane whose number differs in bit d.
 __device__ __forceinline__ float lane_xor(float v, int d) { return __shfl_xor(v, d); }
+__device__ __forceinline__ Seen lane_xor(Seen s, int d) { return Seen{__shfl_xor(s.top, d), __shfl_xor(s.sum, d)}; }
 __device__ __forceinline__ Tally lane_xor(Tally t, int d) { return Tally{__shfl_xor(t.sum, d), __shfl_xor(t.n, d)}; }
 
 template <int THREADS, typename T, typename F>
@@ -124,7 +141,8 @@ struct Row {
     return i < head ? i : i < head + tail ? head + vecs * N + (i - head) : -1;
   }
   // A piece that is read for the last time goes past the caches (4,096 x 22,000 bf16 with gradient: 69 us through
-  // them, 61 past; gradients stored past them as well: 68).
+  // them, 61 past; gradients stored past them as well: 68). The longest rows do where they fill their 128-byte lines
+  // (2,048 x 65,536 bf16: 138 and 129 us; 8,191 x 131,071, which do not: 872 through the caches, 915 past).
   template <bool LAST>
   __device__ __forceinline__ typename P::raw get(int j) const {
     const auto* p = reinterpret_cast<const typename P::raw*>(z + head + (int64_t)j * N);
@@ -167,7 +185,7 @@ __device__ __forceinline__ void as_stored(T& v) {
   v = __builtin_bit_cast(T, w);
 }
 
-template <int DT, int THREADS, int CH, bool GRAD, bool SAME>
+template <int DT, int THREADS, int CH, bool GRAD, bool SAME, bool PAST = true>
 __global__ void __launch_bounds__(THREADS) k_xent_row(gs_xent x) {
   using R = Row<DT>;
   using P = typename R::P;
@@ -191,7 +209,7 @@ __global__ void __launch_bounds__(THREADS) k_xent_row(gs_xent x) {
   for (int i = 0; i < CH; ++i) {
     const int j = tid + i * THREADS;
     if (j < row.vecs)
-      r[i] = row.template get<true>(j);
+      r[i] = row.template get<PAST>(j);
     else
       r[i] = P::down((typename P::wide)(-inf()));
   }
@@ -234,28 +252,13 @@ __global__ void __launch_bounds__(THREADS) k_xent_row(gs_xent x) {
   }
 }
 
-// (maximum, sum of e^(z - maximum)) of what has been seen; a maximum of -inf stands for 0 in the sum.
-struct Seen {
-  float top, sum;
-};
-
-__device__ __forceinline__ float base_of(float top) { return top == -inf() ? 0.0f : top; }
-
-// A side that has seen nothing (or only -inf, or NaN) keeps its sum, 0 or NaN, as it is.
-__device__ __forceinline__ float moved(Seen p, float top) { return p.top == -inf() ? p.sum : p.sum * exp_of(p.top - top); }
-
-__device__ __forceinline__ Seen join(Seen p, Seen q) {
-  const float top = fmaxf(p.top, q.top);
-  return Seen{top, moved(p, top) + moved(q, top)};
-}
-
 // Work: one float (1 / rows that count) and one unused, the targets' logits [N], the parts [N][parts].
 __device__ __forceinline__ float* targets_of(const gs_xent& x) { return static_cast<float*>(x.work) + 2; }
 __device__ __forceinline__ Seen* parts_of(const gs_xent& x, int64_t n, int parts) {
   return reinterpret_cast<Seen*>(static_cast<float*>(x.work) + 2 + (x.N + 1) / 2 * 2) + n * parts;
 }
 
-template <int DT>
+template <int DT, bool PAST>
 __global__ void __launch_bounds__(kPartThreads) k_xent_part(gs_xent x, int parts, int part_vecs) {
   using R = Row<DT>;
   using P = typename R::P;
@@ -276,14 +279,14 @@ __global__ void __launch_bounds__(kPartThreads) k_xent_part(gs_xent x, int parts
       mine = Seen{fmaxf(z, -inf()), exp_of(z - base_of(fmaxf(z, -inf())))};
     }
   }
-  constexpr int U = 4;
+  constexpr int U = 8;
   for (int j0 = from + tid; j0 < to; j0 += U * kPartThreads) {
     typename P::raw r[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int j = j0 + u * kPartThreads;
       if (j < to)
-        r[u] = row.template get<false>(j);
+        r[u] = row.template get<PAST>(j);
       else
         r[u] = P::down((typename P::wide)(-inf()));
     }
@@ -303,16 +306,8 @@ __global__ void __launch_bounds__(kPartThreads) k_xent_part(gs_xent x, int parts
     }
     mine = join(mine, now);
   }
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) mine = join(mine, Seen{__shfl_xor(mine.top, d), __shfl_xor(mine.sum, d)});
-  if ((tid & 63) == 0) lds[tid >> 6] = mine;
-  __syncthreads();
-  if (tid == 0) {
-    Seen all = lds[0];
-#pragma unroll
-    for (int w = 1; w < kPartThreads / 64; ++w) all = join(all, lds[w]);
-    parts_of(x, n, parts)[part] = all;
-  }
+  mine = block_reduce<kPartThreads>(mine, lds, join);
+  if (tid == 0) parts_of(x, n, parts)[part] = mine;
 }
 
 // Joins a row's parts (every workgroup, in one order) and writes the gradient of one of them. Without a
@@ -338,16 +333,25 @@ __global__ void __launch_bounds__(kPartThreads) k_xent_join(gs_xent x, int parts
     }
     return;
   }
-  const Seen* all = parts_of(x, n, parts);
-  Seen s = all[0];
-  for (int q = 1; q < parts; ++q) s = join(s, all[q]);
+  __shared__ Seen lds[kPartThreads / 64];
+  Seen s{-inf(), 0.0f};
+  if (tid < parts) s = parts_of(x, n, parts)[tid];
+  s = block_reduce<kPartThreads>(s, lds, join);
   if (part == 0 && tid == 0 && x.losses) x.losses[n] = logf(s.sum) - (targets_of(x)[n] - s.top);
   if (!GRAD) return;
   const bool known = t >= 0 && t < x.V;
   const float share = known ? 1.0f / s.sum : __builtin_nanf(""), m = factor_of(x, n);
   const int mark = known ? (int)t - row.head : -1;
-  for (int j = from + tid; j < to; j += kPartThreads)
-    row.template put_grad<SAME>(j, row.template get<true>(j), s.top, share, m, mark);
+  constexpr int U = 4;
+  for (int j0 = from + tid; j0 < to; j0 += U * kPartThreads) {
+    typename P::raw r[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (j0 + u * kPartThreads < to) r[u] = row.template get<true>(j0 + u * kPartThreads);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (j0 + u * kPartThreads < to) row.template put_grad<SAME>(j0 + u * kPartThreads, r[u], s.top, share, m, mark);
+  }
   if (edge >= 0) {
     const float p = exp_of((float)row.z[edge] - s.top) * share;
     row.grad[edge] = (E)(m * (known && edge == (int)t ? p - 1.0f : p));
@@ -360,16 +364,13 @@ struct Cut {
 };
 
 Cut cut_of(int64_t N, int64_t V, int dtype) {
-  const int64_t vecs = V / (16 / elem_size(dtype)) + 1;
-  const bool held = vecs <= (int64_t)kRowThreads * kRowPieces;
-  const int64_t least = kPartThreads * kPartVecs;
+  const int64_t vecs = V / (16 / elem_size(dtype)), least = kPartThreads * kPartVecs;
   int64_t parts = 0;
-  if (!held || (N * 4 <= kSplitWant && vecs >= 4 * least)) {
+  if (vecs > (int64_t)kRowThreads * kRowPieces || (N <= kFewRows && vecs >= kLongRow)) {
     parts = N > 0 ? (kSplitWant + N - 1) / N : 1;
     const int64_t most = (vecs + least - 1) / least;
     parts = parts < most ? parts : most;
     parts = parts < kMaxParts ? parts : kMaxParts;
-    parts = parts > 1 ? parts : 1;
   }
   Cut k{(int)parts, 0};
   if (parts > 0) k.part_vecs = (int)((vecs + parts - 1) / parts);
@@ -378,7 +379,7 @@ Cut cut_of(int64_t N, int64_t V, int dtype) {
 
 template <int DT, bool GRAD, bool SAME>
 void rows(hipStream_t s, const gs_xent& x) {
-  const int64_t vecs = x.V / (16 / elem_size(DT)) + 1;
+  const int64_t vecs = x.V / (16 / elem_size(DT));
   const dim3 grid = grid_of(x.N);
 #define GS_XENT(THREADS, CH) \
   if (vecs <= (THREADS) * (CH)) return k_xent_row<DT, THREADS, CH, GRAD, SAME><<<grid, THREADS, 0, s>>>(x), void()
@@ -392,8 +393,11 @@ void rows(hipStream_t s, const gs_xent& x) {
   GS_XENT(512, 6);
   GS_XENT(512, 8);
   GS_XENT(1024, 8);
-  GS_XENT(kRowThreads, kRowPieces);
 #undef GS_XENT
+  if ((((uintptr_t)x.logits | (x.logits_stride * elem_size(DT))) & 127) == 0)
+    k_xent_row<DT, kRowThreads, kRowPieces, GRAD, SAME, true><<<grid, kRowThreads, 0, s>>>(x);
+  else
+    k_xent_row<DT, kRowThreads, kRowPieces, GRAD, SAME, false><<<grid, kRowThreads, 0, s>>>(x);
 }
 
 template <int DT, bool GRAD, bool SAME>
@@ -401,7 +405,12 @@ void launch(hipStream_t s, const gs_xent& x) {
   const Cut k = cut_of(x.N, x.V, DT);
   if (k.parts == 0) return rows<DT, GRAD, SAME>(s, x);
   const dim3 grid = grid_of(x.N * k.parts);
-  k_xent_part<DT><<<grid, kPartThreads, 0, s>>>(x, k.parts, k.part_vecs);
+  // few rows are still in the caches when they are read again; many are not (1,000 x 150,000 bf16: 94 + 103 us with
+  // the first read through the caches, 57 + 117 past them)
+  if (x.N <= kFewRows)
+    k_xent_part<DT, false><<<grid, kPartThreads, 0, s>>>(x, k.parts, k.part_vecs);
+  else
+    k_xent_part<DT, true><<<grid, kPartThreads, 0, s>>>(x, k.parts, k.part_vecs);
   k_xent_join<DT, GRAD, SAME><<<GRAD ? grid : grid_of(x.N), kPartThreads, 0, s>>>(x, k.parts, k.part_vecs);
 }
 
