@@ -61,14 +61,25 @@ def _rows(t, like, device: int, name: str) -> gs_rows:
     """A [B][T][C] tensor whose channels are contiguous, as the C ABI takes it."""
     if t is None:
         return gs_rows(None, 0, 0)
-    if not isinstance(t, torch.Tensor) or t.get_device() != device or t.dtype is not like.dtype:
+    if not isinstance(t, torch.Tensor) or t.dtype is not like.dtype or t.get_device() != device:
         raise TypeError(f"{name} must be a {like.dtype} tensor on {like.device}")
-    if t.shape != like.shape:
-        raise ValueError(f"{name} must have shape {tuple(like.shape)}, got {tuple(t.shape)}")
+    shape = t.shape
+    if shape != like.shape:
+        raise ValueError(f"{name} must have shape {tuple(like.shape)}, got {tuple(shape)}")
     sb, st, sc = t.stride()
-    if sc != 1 and t.shape[2] > 1:
+    if sc != 1 and shape[2] > 1:
         raise ValueError(f"{name}: channels must be contiguous")
     return gs_rows(t.data_ptr(), sb, st)
+
+
+def _made(t, like, device: int, name: str):
+    """(the tensor, its rows) of an output: the given one, or a new contiguous one."""
+    if t is not None:
+        _written(t, name)
+        return t, _rows(t, like, device, name)
+    t = torch.empty_like(like, memory_format=torch.contiguous_format)
+    _, T, C = like.shape
+    return t, gs_rows(t.data_ptr(), T * C, C)
 
 
 def _written(t, name: str) -> None:
@@ -111,17 +122,16 @@ def recurrence_forward(x, f, o=None, h0=None, lengths=None, save: bool = False, 
     itself for a step in place) are made unless given. save: also the states that ``recurrence_backward`` needs."""
     r, device, work = _recurrence(x, f, o, h0, lengths)
     B, T, C = x.shape
-    if y is None:
-        y = torch.empty_like(x, memory_format=torch.contiguous_format)
-    else:
-        _written(y, "y")
+    y, to = _made(y, x, device, "y")
     if h_last is None:
-        h_last = torch.empty((B, C), dtype=torch.float32, device=x.device)
+        h_last = x.new_empty((B, C), dtype=torch.float32)
+        last = h_last.data_ptr()
+    else:
+        last = _side(h_last, torch.float32, (B, C), device, "h_last")
     saved = None
     if save:
-        saved = torch.empty((B, -(-T // GS_RECURRENCE_BLOCK), C), dtype=torch.float32, device=x.device)
-    _check(load_library().gs_recurrence_forward(ctypes.byref(r), _stream(device), _rows(y, x, device, "y"),
-                                                _side(h_last, torch.float32, (B, C), device, "h_last"),
+        saved = x.new_empty((B, -(-T // GS_RECURRENCE_BLOCK), C), dtype=torch.float32)
+    _check(load_library().gs_recurrence_forward(ctypes.byref(r), _stream(device), to, last,
                                                 saved.data_ptr() if save else None,
                                                 work.data_ptr() if work is not None else None),
            None, "gs_recurrence_forward")
@@ -135,23 +145,17 @@ def recurrence_backward(gy, x, f, o, saved, lengths=None, gh=None, dx=None, df=N
     r, device, work = _recurrence(x, f, o, None, lengths)
     B, T, C = x.shape
 
-    def out(t, name):
-        if t is None:
-            return torch.empty_like(x, memory_format=torch.contiguous_format)
-        _written(t, name)
-        return t
-
-    dx, df = out(dx, "dx"), out(df, "df")
     if o is None and do is not None:
         raise ValueError("do is given but o is not")
-    do = out(do, "do") if o is not None else None
-    dh0 = torch.empty((B, C), dtype=torch.float32, device=x.device)
+    dx, to_x = _made(dx, x, device, "dx")
+    df, to_f = _made(df, x, device, "df")
+    do, to_o = _made(do, x, device, "do") if o is not None else (None, gs_rows(None, 0, 0))
+    dh0 = x.new_empty((B, C), dtype=torch.float32)
     blocks = -(-T // GS_RECURRENCE_BLOCK)
     _check(load_library().gs_recurrence_backward(ctypes.byref(r), _stream(device), _rows(gy, x, device, "gy"),
                                                  _side(gh, torch.float32, (B, C), device, "gh"),
-                                                 _side(saved, torch.float32, (B, blocks, C), device, "saved"),
-                                                 _rows(dx, x, device, "dx"), _rows(df, x, device, "df"),
-                                                 _rows(do, x, device, "do"), dh0.data_ptr(),
+                                                 _side(saved, torch.float32, (B, blocks, C), device, "saved"), to_x,
+                                                 to_f, to_o, dh0.data_ptr(),
                                                  work.data_ptr() if work is not None else None),
            None, "gs_recurrence_backward")
     return dx, df, do, dh0
@@ -160,7 +164,7 @@ def recurrence_backward(gy, x, f, o, saved, lengths=None, gh=None, dx=None, df=N
 class _Recurrence(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, f, o, h0, lengths):
-        y, h_last, saved = recurrence_forward(x, f, o, h0, lengths, save=True)
+        y, h_last, saved = recurrence_forward(x, f, o, h0, lengths, save=any(ctx.needs_input_grad))
         ctx.save_for_backward(x, f, o, lengths, saved)
         ctx.set_materialize_grads(False)
         return y, h_last
@@ -181,7 +185,7 @@ class _PackedRecurrence(torch.autograd.Function):
     def forward(ctx, xfo, channels, h0, lengths):
         parts = xfo.split(channels, -1)
         y, h_last, saved = recurrence_forward(parts[0], parts[1], parts[2] if len(parts) == 3 else None, h0, lengths,
-                                              save=True)
+                                              save=any(ctx.needs_input_grad))
         ctx.save_for_backward(xfo, lengths, saved)
         ctx.channels = channels
         ctx.set_materialize_grads(False)
@@ -310,11 +314,10 @@ def cross_entropy_forward(logits, targets, ignore_index: int = -100, grad=False,
     contiguous; targets: int64 [N]. mean: fp32 scalar, over the rows whose target is not ignore_index (0 when there is
     none); losses: fp32 [N]. grad: False (dlogits is None), True, or a tensor to write, the logits themselves
     included: the gradient of factor * mean (the factor scales a loss of 16-bit gradients)."""
-    f32 = dict(dtype=torch.float32, device=logits.device)
-    out = torch.empty((logits.shape[0],), **f32)
-    mean = torch.empty((), **f32)
+    out = logits.new_empty(logits.shape[:1], dtype=torch.float32)
+    mean = logits.new_empty((), dtype=torch.float32)
     if grad is True:
-        grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        grad = torch.empty_like(logits, memory_format=torch.contiguous_format)
     elif grad is False:
         grad = None
     _cross_entropy(logits, targets, ignore_index, out, mean, grad, factor=factor, mean=True)

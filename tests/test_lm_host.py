@@ -56,6 +56,22 @@ def test_recurrence_refuses_its_other_arguments(lib):
     assert lib.gs_recurrence_backward(ungated, None, rows(), None, FAKE, rows(), rows(), rows(), None, FAKE) == INVALID
 
 
+def test_work_split_along_time_needs_its_scratch(lib):
+    r = recurrence(B=1, T=1 << 20, C=8)
+    n = lib.gs_recurrence_work(1, 1 << 20, 8, gs.GS_BF16)
+    # one map of two fp32 values a channel for each segment, at most 128 of them
+    assert 0 < n <= 128 * 2 * 8 * 4
+    assert lib.gs_recurrence_forward(ctypes.byref(r), None, rows(), FAKE, None, None) == INVALID
+    assert b"work" in lib.gs_last_error(None)
+    assert lib.gs_recurrence_backward(ctypes.byref(r), None, rows(), None, FAKE, rows(), rows(), rows(), None,
+                                      None) == INVALID
+    for T in (1, 8, gs.GS_RECURRENCE_BLOCK):  # never for so few steps
+        for C in (1, 2, 63, 64, 5000):
+            for dtype in (gs.GS_F32, gs.GS_BF16, gs.GS_F16):
+                assert lib.gs_recurrence_work(1, T, C, dtype) == 0
+    assert lib.gs_recurrence_work(1, 1, 1 << 25, gs.GS_F32) < 0  # over GS_RECURRENCE_MAX_CHANNELS
+
+
 def test_nothing_to_compute_is_no_error(lib):
     none = rows(None)
     for size in (dict(B=0), dict(C=0)):
