@@ -41,12 +41,12 @@ struct Pack {
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // sigmoid(z) and 1 - sigmoid(z) = sigmoid(-z), each to a few ulp of itself (1 - s would lose the
-// digits of a gate near one): with e = exp(-|z|) they are 1 / (1 + e) and e / (1 + e).
+// digits of a gate near one): with e = exp(-z) they are 1 / (1 + e) and e / (1 + e). The exponent stops at 2^126, where
+// the first is 2^-126 and the second 1, so that no gate of any size is infinity times zero; the minimum keeps a NaN.
 __device__ __forceinline__ void sigmoid_both(float z, float& s, float& rest) {
-  const float e = __builtin_amdgcn_exp2f(-fabsf(z) * kLog2e);
-  const float big = __builtin_amdgcn_rcpf(1.0f + e), small = e * big;
-  s = z >= 0.0f ? big : small;
-  rest = z >= 0.0f ? small : big;
+  const float e = __builtin_amdgcn_exp2f(__builtin_elementwise_minimum(-z * kLog2e, 126.0f));
+  s = __builtin_amdgcn_rcpf(1.0f + e);
+  rest = e * s;
 }
 
 __device__ __forceinline__ float sigmoid_of(float z) {

@@ -211,7 +211,7 @@ __global__ void __launch_bounds__(W* G, G > 1 ? 4 : 1) k_recurrence_fwd(Recurren
   __shared__ V maps[G > 1 ? 2 : 1][2][G][W];
   const Place p = place_of<(G > 1)>(cut, cut.segs - (REDUCE ? 1 : 0), 0, a.B);
   if (p.b >= a.B) return;
-  const int lane = threadIdx.x % W, g = threadIdx.x / W;
+  const int lane = threadIdx.x % W, g = W == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / W) : threadIdx.x / W;
   const int64_t c0 = (int64_t)p.strip * (W * VEC);
   const bool live = c0 + lane * VEC < a.C;
   const int64_t c = live ? c0 + lane * VEC : a.C - VEC;  // for lanes past the last channel another one's state
@@ -328,7 +328,7 @@ __global__ void __launch_bounds__(W* G, G == 4 ? 3 : G == 8 ? 2 : 1) k_recurrenc
   __shared__ V maps[G > 1 ? 2 : 1][3][G][W];
   const Place p = place_of<(G > 1)>(cut, cut.segs - (REDUCE ? 1 : 0), REDUCE ? 1 : 0, a.B);
   if (p.b >= a.B) return;
-  const int lane = threadIdx.x % W, g = threadIdx.x / W;
+  const int lane = threadIdx.x % W, g = W == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / W) : threadIdx.x / W;
   const int64_t c0 = (int64_t)p.strip * (W * VEC);
   const bool live = c0 + lane * VEC < a.C;
   const int64_t c = live ? c0 + lane * VEC : a.C - VEC;
