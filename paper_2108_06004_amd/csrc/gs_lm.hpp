@@ -41,12 +41,12 @@ struct Pack {
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // sigmoid(z) and 1 - sigmoid(z) = sigmoid(-z), each to a few ulp of itself (1 - s would lose the
-// digits of a gate near one): with e = exp(-z) they are 1 / (1 + e) and e / (1 + e). The exponent stops at 2^126, where
-// the first is 2^-126 and the second 1, so that no gate of any size is infinity times zero; the minimum keeps a NaN.
+// digits of a gate near one): with e = exp(-z) they are 1 / (1 + e) and e / (1 + e). Where e is so large that
+// the first is 0 or no normal number the second is 1 (e may be infinite there); a NaN stays one.
 __device__ __forceinline__ void sigmoid_both(float z, float& s, float& rest) {
-  const float e = __builtin_amdgcn_exp2f(__builtin_elementwise_minimum(-z * kLog2e, 126.0f));
+  const float e = __builtin_amdgcn_exp2f(-z * kLog2e);
   s = __builtin_amdgcn_rcpf(1.0f + e);
-  rest = e * s;
+  rest = s < 0x1p-125f ? 1.0f : e * s;
 }
 
 __device__ __forceinline__ float sigmoid_of(float z) {

@@ -120,6 +120,20 @@ def test_recurrence_extreme_gates():
         run_and_check(i, what=str(dtype))
 
 
+def test_recurrence_nan_gates_are_not_swallowed():
+    # a NaN among the tokens reaches everything computed from it, and nothing else
+    for T, t in ((1, 0), (6, 2), (200, 70), (3000, 1500)):
+        i = inputs(4, 2, T, 70, torch.bfloat16)
+        i["f"][1, t, 5] = NAN
+        y, h, saved = lm.recurrence_forward(i["x"], i["f"], i["o"], h0=i["h0"], save=True)
+        dx, df, do, dh0 = lm.recurrence_backward(i["gy"], i["x"], i["f"], i["o"], saved, gh=i["gh"])
+        assert torch.isnan(y[1, t:, 5]).all() and torch.isnan(h[1, 5]) and torch.isnan(dh0[1, 5])
+        assert torch.isnan(do[1, t:, 5]).all() and torch.isnan(df[1, :t + 1, 5]).all() and torch.isnan(dx[1, :t, 5]).all()
+        for out in (y, dx, df, do):
+            assert torch.isfinite(out[0]).all() and torch.isfinite(out[1, :, 6:]).all() and torch.isfinite(out[1, :, :5]).all()
+        assert torch.isfinite(y[1, :t, 5]).all()
+
+
 def test_recurrence_zero_sizes():
     for B, T, C in ((0, 5, 8), (3, 0, 8), (3, 5, 0)):
         i = inputs(1, B, T, C, torch.bfloat16)
