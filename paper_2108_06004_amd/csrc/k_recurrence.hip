@@ -79,11 +79,10 @@ __device__ __forceinline__ Place place_of(const Cut& k, unsigned parts, int from
 // GS_RECURRENCE_MAX_STRIDE fp32 elements, 128 channels). Offset kNowhere is out of the buffer's range: a load
 // there gives zero and a store is dropped, so steps and channels that are not there need no branches.
 constexpr uint32_t kNowhere = 0x80000000u;
-// Cache policies: through the caches, or past them (non-temporal). Rows that start and end on 128-byte lines are read
-// and reduced past the caches (16 x 4,096 x 2,048 bf16 forward 243 us through them, 220 past; reducing 1 x 65,536 x
-// 1,024 75 and 49), rows that share lines with their neighbours through them (64 x 512 x 1,500: 89 and 95). y is
-// stored past them (64 x 512 x 1,500: 106 us through them, 89 past), gradients through them (219 us past, 146
-// through).
+// Cache policies: through the caches, or past them (non-temporal). Rows that start and end on 128-byte lines go past
+// them in both directions (16 x 4,096 x 2,048 bf16, both directions: 580 us, 603 with the gradients' pass through
+// them), rows that share lines with their neighbours through them (64 x 512 x 1,500: 276 us, 306 past), but for
+// y, which is stored past them (1 x 65,536 x 1,024: 440 us, 455 through them).
 constexpr int kCached = 0, kPast = 2;
 
 struct Block {
@@ -448,9 +447,9 @@ __global__ void __launch_bounds__(W* G, G == 4 ? 3 : G == 8 ? 2 : 1) k_recurrenc
       const V dx = rest[i] * q[i], df = (dx * k[i]) * (h - xi);  // padding: rest and shut are 0
       h = join<VEC>(k[i], h, rest[i] * xi);
       const bool in = FULL || t0 + first + i < T;
-      store<DT, VEC, kCached>(to_x, in ? at_x : kNowhere, i, dx);
-      store<DT, VEC, kCached>(to_f, in ? at_f : kNowhere, i, df);
-      if (GATE) store<DT, VEC, kCached>(to_o, in ? at_o : kNowhere, i, shut[i] * h);
+      store<DT, VEC, AUX>(to_x, in ? at_x : kNowhere, i, dx);
+      store<DT, VEC, AUX>(to_f, in ? at_f : kNowhere, i, df);
+      if (GATE) store<DT, VEC, AUX>(to_o, in ? at_o : kNowhere, i, shut[i] * h);
     }
   };
   int blk = p.blk1 - 1;
@@ -492,12 +491,13 @@ constexpr int kSteps = 8;           // of a thread
 constexpr int kChip = 256;          // workgroups that give every CU one
 constexpr int kMaxSegs = 128;
 
-// How a direction is cut. Single tokens and up to eight steps need no groups. More steps take eight groups a
-// workgroup; the backward pass, which needs 1.7 times the registers, takes four where that still gives the
-// CUs more than one workgroup each (16 x 4,096 x 2,048 bf16, 256 workgroups: 490 us with four groups, 412 with
-// eight). At most half a workgroup a CU: time is split to two a CU, which costs reading two or three arrays twice
-// (1 x 65,536 x 1,024: 256 workgroups 178 us forward, 512 160, 1,024 175), to four where a segment would be
-// shorter than eight blocks (5 x 1,037 x 1,500 fp16: 34 us with two a CU, 27 with four).
+// How a direction is cut. Single tokens and up to eight steps need no groups; more steps take eight groups a workgroup.
+// Up to one workgroup a CU the forward pass takes sixteen, for more waves on each (16 x 4,096 x 2,048 bf16, 256
+// workgroups: 223 us with eight, 210 with sixteen; 32 x 512 x 1,500, 384: 56 and 60). The backward pass needs 1.6 times
+// the registers and takes four where that still gives the CUs more than one workgroup each (256 workgroups:
+// 490 us with four, 412 with eight). At most half a workgroup a CU: time is split to two a CU, which costs reading
+// two or three arrays twice (1 x 65,536 x 1,024: 256 workgroups 178 us forward, 512 160, 1,024 175), to four where a
+// segment would be shorter than eight blocks (5 x 1,037 x 1,500 fp16: 34 us with two a CU, 27 with four).
 Cut cut_of(int64_t B, int64_t T, int64_t C, int vec, bool backward) {
   Cut k{};
   k.strips = (unsigned)((C + 64 * vec - 1) / (64 * vec));
@@ -505,7 +505,12 @@ Cut cut_of(int64_t B, int64_t T, int64_t C, int vec, bool backward) {
   k.segs = 1;
   const int64_t have = B * (int64_t)k.strips;
   const bool split = T > kSteps && 2 * have <= kChip;
-  k.groups = T <= kSteps ? 1 : backward && (split || 4 * have > 5 * kChip) ? 4 : 8;
+  if (T <= kSteps)
+    k.groups = 1;
+  else if (backward)
+    k.groups = split || 4 * have > 5 * kChip ? 4 : 8;
+  else
+    k.groups = split || have > kChip ? 8 : 16;
   const int64_t span = T <= 1 ? 1 : k.groups * kSteps;
   k.all = (int)((T + span - 1) / span);
   k.seg_blocks = k.all;
@@ -526,6 +531,10 @@ void forward(hipStream_t s, const RecurrenceArgs& a, const Cut& k, dim3 grid, bo
     k_recurrence_fwd<DT, VEC, GATE, 64, 1, 1, false, kCached><<<grid, 64, 0, s>>>(a, k);
   else if (k.groups == 1)
     k_recurrence_fwd<DT, VEC, GATE, 64, 1, kSteps, false, kCached><<<grid, 64, 0, s>>>(a, k);
+  else if (k.groups == 16 && lines)
+    k_recurrence_fwd<DT, VEC, GATE, 64, 16, kSteps, false, kPast><<<grid, 1024, 0, s>>>(a, k);
+  else if (k.groups == 16)
+    k_recurrence_fwd<DT, VEC, GATE, 64, 16, kSteps, false, kCached><<<grid, 1024, 0, s>>>(a, k);
   else if (lines)
     k_recurrence_fwd<DT, VEC, GATE, 64, 8, kSteps, REDUCE, kPast><<<grid, 512, 0, s>>>(a, k);
   else
@@ -538,10 +547,12 @@ void backward(hipStream_t s, const RecurrenceArgs& a, const Cut& k, dim3 grid, b
     k_recurrence_bwd<DT, VEC, GATE, 64, 1, 1, false, kCached><<<grid, 64, 0, s>>>(a, k);
   else if (k.groups == 1)
     k_recurrence_bwd<DT, VEC, GATE, 64, 1, kSteps, false, kCached><<<grid, 64, 0, s>>>(a, k);
+  else if (k.groups == 8 && lines)
+    k_recurrence_bwd<DT, VEC, GATE, 64, 8, kSteps, false, kPast><<<grid, 512, 0, s>>>(a, k);
   else if (k.groups == 8)
     k_recurrence_bwd<DT, VEC, GATE, 64, 8, kSteps, false, kCached><<<grid, 512, 0, s>>>(a, k);
-  else if (REDUCE && lines)
-    k_recurrence_bwd<DT, VEC, GATE, 64, 4, kSteps, REDUCE, REDUCE ? kPast : kCached><<<grid, 256, 0, s>>>(a, k);
+  else if (lines)
+    k_recurrence_bwd<DT, VEC, GATE, 64, 4, kSteps, REDUCE, kPast><<<grid, 256, 0, s>>>(a, k);
   else
     k_recurrence_bwd<DT, VEC, GATE, 64, 4, kSteps, REDUCE, kCached><<<grid, 256, 0, s>>>(a, k);
 }
@@ -612,7 +623,7 @@ hipError_t launch_recurrence_backward(hipStream_t s, int dtype, const Recurrence
                                  pairs(a.df, bytes) && (!a.o.p || (pairs(a.o, bytes) && pairs(a.dout, bytes))))) &&
                    pairs(a.gh) && pairs(a.dh0) && pairs(a.states) && pairs(a.work);
   const Cut k = cut_of(a.B, a.T, a.C, two ? 2 : 1, true);
-  const bool whole = lines(a.gy) && lines(a.f) && lines(a.o);
+  const bool whole = lines(a.x) && lines(a.f) && lines(a.o) && lines(a.gy) && lines(a.dx) && lines(a.df) && lines(a.dout);
   with_type(dtype, two, a.o.p != nullptr, [&](auto dt, auto vec, auto gate) {
     constexpr int DT = decltype(dt)::value, VEC = decltype(vec)::value;
     constexpr bool GATE = decltype(gate)::value;
