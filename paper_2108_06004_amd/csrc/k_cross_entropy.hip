@@ -213,14 +213,17 @@ __global__ void __launch_bounds__(THREADS) k_xent_row(gs_xent x) {
     }
     return;
   }
-  typename P::raw r[CH];
+struct Piece {  // in a struct: the compiler makes one long vector of a plain array (8 fp32 pieces: 252 registers for 64)
+    typename P::raw v;
+  };
+  Piece r[CH];
 #pragma unroll
   for (int i = 0; i < CH; ++i) {
     const int j = tid + i * THREADS;
     if (j < row.vecs)
-      r[i] = row.template get<PAST>(j);
+      r[i].v = row.template get<PAST>(j);
     else
-      r[i] = P::down((typename P::wide)(-inf()));
+      r[i].v = P::down((typename P::wide)(-inf()));
   }
   const float side = edge >= 0 ? (float)row.z[edge] : -inf();
   const bool known = t >= 0 && t < x.V;
@@ -230,7 +233,7 @@ __global__ void __launch_bounds__(THREADS) k_xent_row(gs_xent x) {
 #pragma unroll
   for (int i = 0; i < CH; ++i)
     if (i * THREADS < row.vecs) {
-      const typename P::wide v = P::up(r[i]);
+      const typename P::wide v = P::up(r[i].v);
 #pragma unroll
       for (int e = 0; e < R::N; ++e) top = fmaxf(top, v[e]);
     }
@@ -239,8 +242,8 @@ __global__ void __launch_bounds__(THREADS) k_xent_row(gs_xent x) {
 #pragma unroll
   for (int i = 0; i < CH; ++i)
     if (i * THREADS < row.vecs) {
-      as_stored(r[i]);
-      const typename P::wide v = P::up(r[i]);
+      as_stored(r[i].v);
+      const typename P::wide v = P::up(r[i].v);
 #pragma unroll
       for (int e = 0; e < R::N; ++e) sum += exp_of(v[e] - top);
     }
@@ -252,8 +255,8 @@ __global__ void __launch_bounds__(THREADS) k_xent_row(gs_xent x) {
 #pragma unroll
   for (int i = 0; i < CH; ++i) {
     const int j = tid + i * THREADS;
-    as_stored(r[i]);
-    if (j < row.vecs) row.template put_grad<SAME>(j, r[i], top, share, m, mark);
+    as_stored(r[i].v);
+    if (j < row.vecs) row.template put_grad<SAME>(j, r[i].v, top, share, m, mark);
   }
   if (edge >= 0) {
     const float p = exp_of(side - top) * share;
