@@ -203,6 +203,41 @@ __device__ __forceinline__ float* slot_of(float* work, const Cut& k, int64_t b, 
   return work + ((b * k.segs + s) * 2) * C;
 }
 
+// The state (going backward: the carry) that `count` slots give from zero, slot first, first + by, ... in that
+// order: each group joins a part of them, four loads of a slot's map at a time, and every thread the groups' maps.
+template <int VEC, int W, int G>
+__device__ __forceinline__ typename Pack<GS_F32, VEC>::wide join_slots(
+    const float* slots, int64_t C, int first, int by, int count, int g, int lane,
+    typename Pack<GS_F32, VEC>::wide (&maps)[G][W], typename Pack<GS_F32, VEC>::wide (&results)[G][W]) {
+  using V = typename Pack<GS_F32, VEC>::wide;
+  const int per = (count + G - 1) / G, end = (g + 1) * per < count ? (g + 1) * per : count;
+  V A = (V)1.0f, S = (V)0.0f;
+  for (int s0 = g * per; s0 < end; s0 += 4) {
+    V a[4], b[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (s0 + u < end) {
+        const float* m = slots + (int64_t)(first + by * (s0 + u)) * 2 * C;
+        a[u] = loadf<VEC>(m);
+        b[u] = loadf<VEC>(m + C);
+      }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (s0 + u < end) {
+        A = A * a[u];
+        S = join<VEC>(a[u], S, b[u]);
+      }
+  }
+  maps[g][lane] = A;
+  results[g][lane] = S;
+  __syncthreads();
+  V h = (V)0.0f;
+#pragma unroll
+  for (int s = 0; s < G; ++s) h = join<VEC>(maps[s][lane], h, results[s][lane]);
+  __syncthreads();  // the blocks use the same memory
+  return h;
+}
+
 template <int DT, int VEC, bool GATE, int W, int G, int L, bool REDUCE, int AUX>
 __global__ void __launch_bounds__(W* G, G > 1 ? 4 : 1) k_recurrence_fwd(RecurrenceArgs a, Cut cut) {
   using V = typename Pack<GS_F32, VEC>::wide;
@@ -223,11 +258,8 @@ __global__ void __launch_bounds__(W* G, G > 1 ? 4 : 1) k_recurrence_fwd(Recurren
       storef<VEC>(slot_of(a.work, cut, p.b, 0, a.C) + c, (V)0.0f);
       storef<VEC>(slot_of(a.work, cut, p.b, 0, a.C) + a.C + c, a.h0 ? loadf<VEC>(a.h0 + p.b * a.C + c) : (V)0.0f);
     }
-  } else if (cut.segs > 1) {
-    for (int s = 0; s <= p.seg; ++s) {
-      const float* m = slot_of(a.work, cut, p.b, s, a.C) + c;
-      h = join<VEC>(loadf<VEC>(m), h, loadf<VEC>(m + a.C));
-    }
+  } else if (G > 1 && cut.segs > 1) {
+    h = join_slots<VEC, W, G>(slot_of(a.work, cut, p.b, 0, a.C) + c, a.C, 0, 1, p.seg + 1, g, lane, maps[0][0], maps[0][1]);
   } else if (a.h0) {
     h = loadf<VEC>(a.h0 + p.b * a.C + c);
   }
@@ -341,11 +373,9 @@ __global__ void __launch_bounds__(W* G, G == 4 ? 3 : G == 8 ? 2 : 1) k_recurrenc
       storef<VEC>(m, (V)0.0f);
       storef<VEC>(m + a.C, a.gh ? loadf<VEC>(a.gh + p.b * a.C + c) : (V)0.0f);
     }
-  } else if (cut.segs > 1) {
-    for (int s = cut.segs - 1; s >= p.seg; --s) {
-      const float* m = slot_of(a.work, cut, p.b, s, a.C) + c;
-      carry = join<VEC>(loadf<VEC>(m), carry, loadf<VEC>(m + a.C));
-    }
+  } else if (G > 1 && cut.segs > 1) {
+    carry = join_slots<VEC, W, G>(slot_of(a.work, cut, p.b, 0, a.C) + c, a.C, cut.segs - 1, -1, cut.segs - p.seg, g, lane,
+                                  maps[0][0], maps[0][1]);
   } else if (a.gh) {
     carry = loadf<VEC>(a.gh + p.b * a.C + c);
   }
