@@ -336,6 +336,7 @@ typedef struct gs_rows {
  * GS_RECURRENCE_MAX_STRIDE. */
 #define GS_RECURRENCE_BLOCK 32
 #define GS_RECURRENCE_BLOCKS(T) (((T) + GS_RECURRENCE_BLOCK - 1) / GS_RECURRENCE_BLOCK)
+#define GS_RECURRENCE_WHOLE 256 /* up to so many steps time is not split over workgroups */
 #define GS_RECURRENCE_MAX_STRIDE 4194304
 #define GS_RECURRENCE_MAX_CHANNELS 16777216
 typedef struct gs_recurrence {
@@ -351,7 +352,7 @@ typedef struct gs_recurrence {
 } gs_recurrence;
 
 /* Bytes of the `work` scratch of the two calls below at these sizes, for either direction
- * (0, always up to T = GS_RECURRENCE_BLOCK: none is needed and work may be NULL; negative: sizes out
+ * (0, always up to T = GS_RECURRENCE_WHOLE: none is needed and work may be NULL; negative: sizes out
  * of range or an unknown dtype). Its contents need not be set and are not kept for anything. */
 int64_t gs_recurrence_work(int64_t B, int64_t T, int64_t C, int32_t dtype);
 

@@ -43,7 +43,9 @@ def state_stride(P: int) -> int:
 # activation types of the language-model operators, and the recurrence's block of saved states
 GS_F32, GS_BF16, GS_F16 = 0, 1, 2
 GS_RECURRENCE_BLOCK = 32
+GS_RECURRENCE_WHOLE = 256
 GS_RECURRENCE_MAX_STRIDE = 4194304
+GS_RECURRENCE_MAX_CHANNELS = 16777216
 
 
 class GsLibraryMissing(RuntimeError):

@@ -519,22 +519,23 @@ __global__ void __launch_bounds__(W* G, G == 4 ? 3 : G == 8 ? 2 : 1) k_recurrenc
 
 constexpr int kSteps = 8;           // of a thread
 constexpr int kChip = 256;          // workgroups that give every CU one
-constexpr int kMaxSegs = 128;
+constexpr int kMaxSegs = 512;
 
 // How a direction is cut. Single tokens and up to eight steps need no groups; more steps take eight groups a workgroup.
 // Up to one workgroup a CU the forward pass takes sixteen, for more waves on each (16 x 4,096 x 2,048 bf16, 256
 // workgroups: 223 us with eight, 210 with sixteen; 32 x 512 x 1,500, 384: 56 and 60). The backward pass needs 1.6 times
 // the registers and takes four where that still gives the CUs more than one workgroup each (256 workgroups:
 // 490 us with four, 412 with eight). At most half a workgroup a CU: time is split to two a CU, which costs reading
-// two or three arrays twice (1 x 65,536 x 1,024: 256 workgroups 178 us forward, 512 160, 1,024 175), to four where a
-// segment would be shorter than eight blocks (5 x 1,037 x 1,500 fp16: 34 us with two a CU, 27 with four).
+// two or three arrays twice (1 x 65,536 x 1,024, both directions: 405 us with two a CU, 441 with four), to four where a
+// segment would be shorter than eight blocks (5 x 1,037 x 1,500 fp16: 34 us with two a CU, 27 with four). Few steps are
+// done in one kernel all the same (1 x 832, both directions: 200 steps 28 us whole, 37 split, 400 steps 48 and 36).
 Cut cut_of(int64_t B, int64_t T, int64_t C, int vec, bool backward) {
   Cut k{};
   k.strips = (unsigned)((C + 64 * vec - 1) / (64 * vec));
   k.blocks = (int)GS_RECURRENCE_BLOCKS(T);
   k.segs = 1;
   const int64_t have = B * (int64_t)k.strips;
-  const bool split = T > kSteps && 2 * have <= kChip;
+  const bool split = T > GS_RECURRENCE_WHOLE && 2 * have <= kChip;
   if (T <= kSteps)
     k.groups = 1;
   else if (backward)

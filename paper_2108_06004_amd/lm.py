@@ -23,7 +23,7 @@ import ctypes
 
 import torch
 
-from . import (GS_BF16, GS_F16, GS_F32, GS_RECURRENCE_BLOCK, _check, gs_recurrence, gs_rows, gs_xent,
+from . import (GS_BF16, GS_F16, GS_F32, GS_RECURRENCE_BLOCK, GS_RECURRENCE_WHOLE, _check, gs_recurrence, gs_rows, gs_xent,
                load_library)
 
 DTYPES = {torch.float32: GS_F32, torch.bfloat16: GS_BF16, torch.float16: GS_F16}
@@ -107,7 +107,7 @@ def _recurrence(x, f, o, h0, lengths):
                       _side(lengths, torch.int32, (B,), device, "lengths"),
                       _side(h0, torch.float32, (B, C), device, "h0"))
     work = None
-    if T > GS_RECURRENCE_BLOCK:
+    if T > GS_RECURRENCE_WHOLE:
         n = load_library().gs_recurrence_work(B, T, C, code)
         work = torch.empty(n, dtype=torch.uint8, device=x.device) if n > 0 else None
     return r, device, work

@@ -59,13 +59,13 @@ def test_recurrence_refuses_its_other_arguments(lib):
 def test_work_split_along_time_needs_its_scratch(lib):
     r = recurrence(B=1, T=1 << 20, C=8)
     n = lib.gs_recurrence_work(1, 1 << 20, 8, gs.GS_BF16)
-    # one map of two fp32 values a channel for each segment, at most 128 of them
-    assert 0 < n <= 128 * 2 * 8 * 4
+    # one map of two fp32 values a channel for each segment, at most 512 of them
+    assert 0 < n <= 512 * 2 * 8 * 4
     assert lib.gs_recurrence_forward(ctypes.byref(r), None, rows(), FAKE, None, None) == INVALID
     assert b"work" in lib.gs_last_error(None)
     assert lib.gs_recurrence_backward(ctypes.byref(r), None, rows(), None, FAKE, rows(), rows(), rows(), None,
                                       None) == INVALID
-    for T in (1, 8, gs.GS_RECURRENCE_BLOCK):  # never for so few steps
+    for T in (1, 8, gs.GS_RECURRENCE_BLOCK, gs.GS_RECURRENCE_WHOLE):  # never for so few steps
         for C in (1, 2, 63, 64, 5000):
             for dtype in (gs.GS_F32, gs.GS_BF16, gs.GS_F16):
                 assert lib.gs_recurrence_work(1, T, C, dtype) == 0
@@ -130,7 +130,8 @@ def test_constants_match_the_header():
 
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     text = open(os.path.join(root, "include", "gs.h")).read()
-    for name in ("GS_F32", "GS_BF16", "GS_F16", "GS_RECURRENCE_BLOCK", "GS_RECURRENCE_MAX_STRIDE"):
+    for name in ("GS_F32", "GS_BF16", "GS_F16", "GS_RECURRENCE_BLOCK", "GS_RECURRENCE_WHOLE", "GS_RECURRENCE_MAX_STRIDE",
+                 "GS_RECURRENCE_MAX_CHANNELS"):
         assert int(re.search(rf"#define {name} (\d+)", text).group(1)) == getattr(gs, name)
 
 
