@@ -594,8 +594,11 @@ dim3 grid_of(const Cut& k, int parts, int64_t B) {
   return dim3((unsigned)(n < kGridX ? n : kGridX), (unsigned)((n + kGridX - 1) / kGridX));
 }
 
-// Two channels a lane for 16-bit elements, where every row of every array starts on a pair of them. fp32 takes one: two
-// need twice the registers for loads (8 x 4,096 x 2,048: 191 + 72 and 423 + 98 us with two, 194 and 390 with one).
+// Two channels a lane for 16-bit elements, where every row of every array starts on a pair of them and one channel a
+// lane would leave a second strip to do. fp32 takes one: two need twice the registers for loads (8 x 4,096 x
+// 2,048: 191 + 72 and 423 + 98 us with two, 194 and 390 with one).
+bool in_pairs(int dtype, int64_t C) { return dtype != GS_F32 && C % 2 == 0 && C > 64; }
+
 bool pairs(const Rows& r, int bytes) {
   const int64_t m = 2 * bytes - 1;
   return ((uintptr_t)r.p & m) == 0 && (r.batch & m) == 0 && (r.time & m) == 0;
@@ -626,14 +629,14 @@ void with_type(int dtype, bool two, bool gate, F f) {
 // For each sequence and segment one map; more segments where a lane takes two channels.
 int64_t recurrence_work(int64_t B, int64_t T, int64_t C, int dtype) {
   if (B == 0 || T == 0 || C == 0) return 0;
-  const int vec = dtype != GS_F32 && C % 2 == 0 ? 2 : 1;
+  const int vec = in_pairs(dtype, C) ? 2 : 1;
   const int f = cut_of(B, T, C, vec, false).segs, b = cut_of(B, T, C, vec, true).segs, segs = f > b ? f : b;
   return segs > 1 ? B * segs * 2 * C * (int64_t)sizeof(float) : 0;
 }
 
 hipError_t launch_recurrence_forward(hipStream_t s, int dtype, const RecurrenceArgs& a) {
   const int bytes = elem_size(dtype);
-  const bool two = dtype != GS_F32 && a.C % 2 == 0 && (a.T == 0 || (pairs(a.x, bytes) && pairs(a.f, bytes) && pairs(a.y, bytes) &&
+  const bool two = in_pairs(dtype, a.C) && (a.T == 0 || (pairs(a.x, bytes) && pairs(a.f, bytes) && pairs(a.y, bytes) &&
                                                  (!a.o.p || pairs(a.o, bytes)))) &&
                    pairs(a.h0) && pairs(a.h_last) && pairs(a.states) && pairs(a.work);
   const Cut k = cut_of(a.B, a.T, a.C, two ? 2 : 1, false);
@@ -649,7 +652,7 @@ hipError_t launch_recurrence_forward(hipStream_t s, int dtype, const RecurrenceA
 
 hipError_t launch_recurrence_backward(hipStream_t s, int dtype, const RecurrenceArgs& a) {
   const int bytes = elem_size(dtype);
-  const bool two = dtype != GS_F32 && a.C % 2 == 0 &&
+  const bool two = in_pairs(dtype, a.C) &&
                    (a.T == 0 || (pairs(a.x, bytes) && pairs(a.f, bytes) && pairs(a.gy, bytes) && pairs(a.dx, bytes) &&
                                  pairs(a.df, bytes) && (!a.o.p || (pairs(a.o, bytes) && pairs(a.dout, bytes))))) &&
                    pairs(a.gh) && pairs(a.dh0) && pairs(a.states) && pairs(a.work);
