@@ -149,19 +149,21 @@ struct Row {
   __device__ __forceinline__ int edge(int i) const {
     return i < head ? i : i < head + tail ? head + vecs * N + (i - head) : -1;
   }
-  // A piece that is read for the last time goes past the caches (4,096 x 22,000 bf16 with gradient: 69 us through
-  // them, 61 past; gradients stored past them as well: 68). The longest rows do where they fill their 128-byte lines
-  // (2,048 x 65,536 bf16: 138 and 129 us; 8,191 x 131,071, which do not: 872 through the caches, 915 past).
-  template <bool LAST>
+  // Pieces read for the last time and gradients go past the caches (PAST; 4,096 x 22,000 bf16 with gradient: 81 us
+  // through them, 78 past; 2,000 x 32,000 fp32 106 and 98), but for the longest rows where they do not fill their
+  // 128-byte lines (8,191 x 131,071 bf16: 873 us through the caches, 902 past).
+  template <bool PAST>
   __device__ __forceinline__ typename P::raw get(int j) const {
     const auto* p = reinterpret_cast<const typename P::raw*>(z + head + (int64_t)j * N);
-    return LAST ? __builtin_nontemporal_load(p) : *p;
+    return PAST ? __builtin_nontemporal_load(p) : *p;
   }
   // Gradients need not have the logits' alignment.
-  template <bool SAME>
+  template <bool SAME, bool PAST>
   __device__ __forceinline__ void put(int j, typename P::raw v) const {
     E* g = grad + head + (int64_t)j * N;
-    if (SAME) {
+    if (SAME && PAST) {
+      __builtin_nontemporal_store(v, reinterpret_cast<typename P::raw*>(g));
+    } else if (SAME) {
       *reinterpret_cast<typename P::raw*>(g) = v;
     } else {
 #pragma unroll
@@ -169,7 +171,7 @@ struct Row {
     }
   }
   // A piece of the gradient m (softmax - [v = t]); `at` is t - head.
-  template <bool SAME>
+  template <bool SAME, bool PAST>
   __device__ __forceinline__ void put_grad(int j, typename P::raw r, float top, float share, float m, int at) const {
     typename P::wide v = P::up(r);
 #pragma unroll
@@ -179,7 +181,7 @@ struct Row {
       for (int e = 0; e < N; ++e)
         if (e == at % N) v[e] -= 1.0f;
     }
-    put<SAME>(j, P::down(v * m));
+    put<SAME, PAST>(j, P::down(v * m));
   }
 };
 
@@ -208,7 +210,7 @@ __global__ void __launch_bounds__(THREADS) k_xent_row(gs_xent x) {
   if (t == x.ignore_index) {
     if (tid == 0 && x.losses) x.losses[n] = 0.0f;
     if (GRAD) {
-      for (int j = tid; j < row.vecs; j += THREADS) row.template put<SAME>(j, P::down((typename P::wide)0.0f));
+      for (int j = tid; j < row.vecs; j += THREADS) row.template put<SAME, PAST>(j, P::down((typename P::wide)0.0f));
       if (edge >= 0) row.grad[edge] = (E)0.0f;
     }
     return;
@@ -256,7 +258,7 @@ struct Piece {  // in a struct: the compiler makes one long vector of a plain ar
   for (int i = 0; i < CH; ++i) {
     const int j = tid + i * THREADS;
     as_stored(r[i].v);
-    if (j < row.vecs) row.template put_grad<SAME>(j, r[i].v, top, share, m, mark);
+    if (j < row.vecs) row.template put_grad<SAME, PAST>(j, r[i].v, top, share, m, mark);
   }
   if (edge >= 0) {
     const float p = exp_of(side - top) * share;
@@ -340,7 +342,7 @@ __global__ void __launch_bounds__(kPartThreads) k_xent_join(gs_xent x, int parts
     if (part == 0 && tid == 0 && x.losses) x.losses[n] = 0.0f;
     if (GRAD) {
       for (int j = from + tid; j < to; j += kPartThreads)
-        row.template put<SAME>(j, P::down((typename P::wide)0.0f));
+        row.template put<SAME, true>(j, P::down((typename P::wide)0.0f));
       if (edge >= 0) row.grad[edge] = (E)0.0f;
     }
     return;
@@ -362,7 +364,7 @@ __global__ void __launch_bounds__(kPartThreads) k_xent_join(gs_xent x, int parts
       if (j0 + u * kPartThreads < to) r[u] = row.template get<true>(j0 + u * kPartThreads);
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (j0 + u * kPartThreads < to) row.template put_grad<SAME>(j0 + u * kPartThreads, r[u], s.top, share, m, mark);
+      if (j0 + u * kPartThreads < to) row.template put_grad<SAME, true>(j0 + u * kPartThreads, r[u], s.top, share, m, mark);
   }
   if (edge >= 0) {
     const float p = exp_of((float)row.z[edge] - s.top) * share;
