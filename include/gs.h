@@ -359,7 +359,8 @@ int64_t gs_recurrence_work(int64_t B, int64_t T, int64_t C, int32_t dtype);
 /* Forward. y: [B][T][C] output. h_last: [B][C] fp32 output, the state after each sequence's last
  * token (h_0 of an empty one); it may be h0's own array. states: [B][GS_RECURRENCE_BLOCKS(T)][C]
  * fp32 output for the backward call, the state before each block of GS_RECURRENCE_BLOCK steps
- * that holds a token, or NULL. */
+ * that holds a token, or NULL. Outputs overlap no input but where said. Time is joined from stretches: a
+ * state that is infinite may become NaN (0 inf) where the gates' product over a stretch is 0 in fp32. */
 gs_status gs_recurrence_forward(const gs_recurrence* r, void* stream, gs_rows y, float* h_last, float* states,
                                 void* work);
 

@@ -6,15 +6,21 @@
 // three times:
 //   - a thread takes L consecutive steps of VEC neighbouring channels. Their loads are all in flight
 //     together (L for each array); it forms its own (A, S) in registers;
-//   - a workgroup of W x G threads takes a strip of W VEC channels and a block of G L = 64 steps, a wave
-//     L of them. The waves' maps go through LDS, every thread joins those before its own and runs its steps
-//     again from registers with the true state. One barrier a block: the maps have two buffers;
+//   - a workgroup of W x G threads takes a strip of W VEC channels and blocks of G L steps (32, 64 or
+//     128), a wave L of them. The waves' maps go through LDS, every thread joins those before its own and runs
+//     its steps again from registers with the true state. One barrier a block: the maps have two buffers. The
+//     next block's loads are under way meanwhile;
 //   - where B and C give too few workgroups, `segs` workgroups share a sequence's blocks. A first
 //     kernel reduces each segment to its map (reading x and f once more), the second starts each segment
 //     from the joined maps before it.
 // The backward pass runs the blocks from the last to the first. s_t = q_t + a_(t+1) s_(t+1) is the
 // same recurrence in reverse, carried as c_t = a_t s_t with the map c -> A c + R; the states are computed
-// again from the state before each block that the forward pass saved (4 / 64 bytes a step).
+// again from the state before every 32 steps that the forward pass saved (an eighth of a byte a step and channel).
+//
+// What bounds it: memory for long inputs (16 x 4,096 x 2,048 bf16: forward 205 us, 5.25 TB/s of its 8 bytes an element,
+// backward 367 us, 5.1 TB/s of 14; VALU 48 and 42% busy, waves waiting for memory half their time). Short
+// ones are bound by the launch (one token of 1,500 channels: 2.8 us). Split along time the reading twice adds to that (1 x
+// 65,536 x 1,024: 47 of 151 us forward, 72 of 254 backward).
 #include <type_traits>
 
 #include "gs_lm.hpp"
@@ -75,9 +81,10 @@ __device__ __forceinline__ Place place_of(const Cut& k, unsigned parts, int from
 }
 
 // One block of a strip of an array as a buffer: its first byte and the strides are the same for the whole
-// workgroup (scalar registers), a thread adds one 32-bit offset, which stays below 2^31 (63 steps of at most
-// GS_RECURRENCE_MAX_STRIDE fp32 elements, 128 channels). Offset kNowhere is out of the buffer's range: a load
-// there gives zero and a store is dropped, so steps and channels that are not there need no branches.
+// workgroup (scalar registers), a thread adds one 32-bit offset, which stays below 2^31 (127 steps of at most
+// GS_RECURRENCE_MAX_STRIDE elements of 32 bits are 127/128 of it, the strip's row less than the rest). Offset
+// kNowhere is out of the buffer's range: a load there gives zero and a store is dropped, so steps and channels
+// that are not there need no branches.
 constexpr uint32_t kNowhere = 0x80000000u;
 // Cache policies: through the caches, or past them (non-temporal). Rows that start and end on 128-byte lines go past
 // them in both directions (16 x 4,096 x 2,048 bf16, both directions: 580 us, 603 with the gradients' pass through
@@ -609,7 +616,6 @@ bool lines(const Rows& r) { return (((uintptr_t)r.p | r.batch | r.time) & 127) =
 
 bool pairs(const float* p) { return ((uintptr_t)p & 7) == 0; }
 
-// Calls f with the element type, the channels of a lane and whether there is an output gate as constants.
 // Calls f with the element type, the channels of a lane and whether there is an output gate as constants.
 template <typename F>
 void with_type(int dtype, bool two, bool gate, F f) {

@@ -57,8 +57,9 @@ def run_and_check(i, lengths=None, what=""):
     return got
 
 
-# one token, the edges of a block of saved states (64), several blocks, an odd number of them
-@pytest.mark.parametrize("T", [1, 2, 7, 8, 9, 16, 17, 63, 64, 65, 127, 128, 129, 300, 1000])
+# one token, a thread's steps (8), the steps between saved states (32), blocks (32, 64, 128) and the length from which
+# time is split (256), each from both sides; several blocks, an odd number of them
+@pytest.mark.parametrize("T", [1, 2, 7, 8, 9, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 300, 1000])
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
 def test_recurrence_lengths_of_time(T, dtype):
     run_and_check(inputs(T, 2, T, 40, dtype), what=f"T={T}")
