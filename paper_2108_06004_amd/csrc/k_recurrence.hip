@@ -481,12 +481,14 @@ __global__ void __launch_bounds__(W* G, G == 4 ? 3 : G == 8 ? 2 : 1) k_recurrenc
 #pragma unroll
     for (int i = 0; i < L; ++i) {
       const V xi = m.x.at(i);
-      const V dx = rest[i] * q[i], df = (dx * k[i]) * (h - xi);  // padding: rest and shut are 0
+      V dx = rest[i] * q[i], df = (dx * k[i]) * (h - xi);
       h = join<VEC>(k[i], h, rest[i] * xi);
+      V dout = GATE ? shut[i] * h : (V)0.0f;
+      if (padded<FULL>(first, i, last)) dx = df = dout = (V)0.0f;  // rest and shut are 0, but h or s may be infinite or NaN
       const bool in = FULL || t0 + first + i < T;
       store<DT, VEC, AUX>(to_x, in ? at_x : kNowhere, i, dx);
       store<DT, VEC, AUX>(to_f, in ? at_f : kNowhere, i, df);
-      if (GATE) store<DT, VEC, AUX>(to_o, in ? at_o : kNowhere, i, shut[i] * h);
+      if (GATE) store<DT, VEC, AUX>(to_o, in ? at_o : kNowhere, i, dout);
     }
   };
   int blk = p.blk1 - 1;

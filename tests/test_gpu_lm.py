@@ -110,6 +110,24 @@ def test_recurrence_padding_is_not_used(B, T, C, lengths, dtype):
         assert not dirty["y"][pad].any() and not dirty["dx"][pad].any() and not dirty["df"][pad].any()
 
 
+@pytest.mark.parametrize("T", [6, 40, 300, 5000])  # no groups, one block, several, split along time
+@pytest.mark.parametrize("gate", [True, False])
+def test_recurrence_gradients_are_zero_at_padding(T, gate):
+    # also where the state or its gradient is infinite or NaN, whose products with zero are not zero
+    for dtype in TYPES:
+        for gh, x in ((float("inf"), 0.0), (NAN, 0.0), (1.0, float("inf")), (1.0, NAN)):
+            i = inputs(T, 4, T, 34, dtype, gate)
+            n = torch.tensor([T - 3, T, 0, T // 2 + 1], dtype=torch.int32, device=DEV)
+            i["gh"][:, ::2] = gh
+            i["x"][:, T // 2, 1::3] += x
+            _, _, saved = lm.recurrence_forward(i["x"], i["f"], i["o"], h0=i["h0"], lengths=n, save=True)
+            dx, df, do, _ = lm.recurrence_backward(i["gy"], i["x"], i["f"], i["o"], saved, lengths=n, gh=i["gh"])
+            pad = torch.arange(T, device=DEV)[None, :] >= n[:, None]
+            for name, t in (("dx", dx), ("df", df), ("do", do)):
+                if t is not None:
+                    assert torch.equal(t[pad], torch.zeros_like(t[pad])), f"{dtype} {name} gh {gh} x {x}"
+
+
 def test_recurrence_extreme_gates():
     # gates of exactly 0 and 1 (infinite pre-activations) and of the types' largest values
     for dtype in TYPES:
