@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(THREADS) k_xent_row(gs_xent x) {
     }
     return;
   }
-struct Piece {  // in a struct: the compiler makes one long vector of a plain array (8 fp32 pieces: 252 registers for 64)
+  struct Piece {  // in a struct: the compiler makes one long vector of a plain array (8 fp32 pieces: 252 registers for 64)
     typename P::raw v;
   };
   Piece r[CH];
