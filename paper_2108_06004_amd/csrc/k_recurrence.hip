@@ -18,9 +18,9 @@
 // again from the state before every 32 steps that the forward pass saved (an eighth of a byte a step and channel).
 //
 // What bounds it: memory for long inputs (16 x 4,096 x 2,048 bf16: forward 205 us, 5.25 TB/s of its 8 bytes an element,
-// backward 367 us, 5.1 TB/s of 14; VALU 48 and 42% busy, waves waiting for memory half their time). Short
+// backward 369 us, 5.1 TB/s of 14; VALU 48 and 42% busy, waves waiting for memory half their time). Short
 // ones are bound by the launch (one token of 1,500 channels: 2.8 us). Split along time the reading twice adds to that (1 x
-// 65,536 x 1,024: 47 of 151 us forward, 72 of 254 backward).
+// 65,536 x 1,024: 47 of 151 us forward, 72 of 256 backward).
 #include <type_traits>
 
 #include "gs_lm.hpp"
