@@ -355,6 +355,35 @@ def cross_entropy(logits, targets, ignore_index: int = -100, reduction: str = "m
     return _CrossEntropy.apply(logits, targets, ignore_index, reduction)
 
 
+# With fp16 activations RecurrentLM.loss_backward multiplies the loss by a power of two up to the number of tokens, this at
+# most: a mean's gradient of the logits, probability / tokens, falls below fp16's smallest number (6e-8) otherwise (2,048
+# tokens of 20,000 words: the embedding's gradient 7% off, the biases of words that do not occur 0). The output projection's
+# gradients, sums over the tokens, are at most this times the largest activation, against fp16's largest number of 65,504.
+HALF_FACTOR = 4096
+
+
+class _Scaled(torch.autograd.Function):
+    """A tensor in another type; its gradient multiplied by a factor, in the tensor's own type."""
+
+    @staticmethod
+    def forward(ctx, t, dtype, factor):
+        ctx.to = (t.dtype, factor)
+        return t.to(dtype)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, g):
+        dtype, factor = ctx.to
+        return g.to(dtype) * factor, None, None
+
+
+def _scaled(t, factor: float, dtype=None):
+    if t is None or (factor == 1.0 and dtype is None):
+        return t
+    dtype = t.dtype if dtype is None else dtype
+    return t.to(dtype) if factor == 1.0 else _Scaled.apply(t, dtype, factor)
+
+
 class RecurrentLM(torch.nn.Module):
     """A language model of these operators: an embedding, layers of projection, gated recurrence and dropout
     onto a residual stream, and an output projection. Parameters are fp32; activations have type ``dtype``.
@@ -377,28 +406,35 @@ class RecurrentLM(torch.nn.Module):
                 layer.bias[width:2 * width] = 1.0  # forget gates start by remembering
         self.register_buffer("step", torch.zeros(1, dtype=torch.int64))
 
-    def _linear(self, layer, u):
-        return torch.nn.functional.linear(u, layer.weight.to(self.dtype), layer.bias.to(self.dtype))
+    def _linear(self, layer, u, factor):
+        return torch.nn.functional.linear(u, _scaled(layer.weight, 1 / factor, self.dtype),
+                                          _scaled(layer.bias, 1 / factor, self.dtype))
 
-    def forward(self, tokens, state=None, lengths=None):
-        """tokens: int64 [B][T]. Returns (logits [B][T][vocab], the state after the tokens)."""
-        u = self.embedding(tokens).to(self.dtype)
+    def forward(self, tokens, state=None, lengths=None, factor: float = 1.0):
+        """tokens: int64 [B][T]. Returns (logits [B][T][vocab], the state after the tokens). factor: what the logits' gradient
+        will come multiplied by (``cross_entropy_forward``'s factor; a power of two costs no rounding). Activations'
+        gradients then hold it, those of parameters and states, which are fp32, do not."""
+        u = _scaled(self.embedding(tokens), 1 / factor, self.dtype)
         after = []
         for j, layer in enumerate(self.inner):
-            y, h = gated_recurrence_packed(self._linear(layer, u), self.width, state[j] if state is not None else None,
-                                           lengths)
-            after.append(h)
+            before = _scaled(state[j], 1 / factor) if state is not None else None
+            y, h = gated_recurrence_packed(self._linear(layer, u, factor), self.width, before, lengths)
+            after.append(_scaled(h, factor))
             if self.training and self.p > 0:
                 u = dropout(y, self.p, self.seed, self.worker * len(self.inner) + j, self.step, residual=u)
             else:
                 u = u + y
-        return self._linear(self.outer, u), after
+        return self._linear(self.outer, u, factor), after
 
     def loss_backward(self, tokens, targets, ignore_index: int = -100):
-        """The mean loss (a detached scalar) of predicting targets ([B][T]); adds its gradient to the parameters."""
-        logits, _ = self(tokens)
+        """The mean loss (a detached scalar) of predicting targets ([B][T]); adds its gradient to the parameters. With
+        fp16 activations the gradient is held at a power of two times itself (``HALF_FACTOR``) on its way to them."""
+        factor = 1.0
+        if self.dtype is torch.float16:
+            factor = float(min(HALF_FACTOR, 1 << max(0, targets.numel().bit_length() - 1)))
+        logits, _ = self(tokens) if factor == 1.0 else self(tokens, factor=factor)
         flat = logits.view(-1, self.vocab)
-        mean, _, grad = cross_entropy_forward(flat.detach(), targets.reshape(-1), ignore_index, grad=True)
+        mean, _, grad = cross_entropy_forward(flat.detach(), targets.reshape(-1), ignore_index, grad=True, factor=factor)
         flat.backward(grad)
         return mean
 

@@ -123,3 +123,63 @@ def test_the_example_learns_its_text():
     # a token's successor follows nine times in ten: log(vocab) = 4.6 before, towards 0.8 after
     got = recurrent_lm.main(["--steps", "80", "--vocab", "100", "--width", "64"])
     assert got["first"] > 4.0 and got["last"] < 0.6 * got["first"] and got["right"] > 0.5
+
+
+def test_gradients_of_a_half_precision_model_of_many_words_and_tokens():
+    # A uniform softmax over 20,000 words, in the mean over 2,048 tokens, is 2.4e-8 an entry of the logits' gradient: less
+    # than half of fp16's smallest number. Every parameter gradient against 64 bits, after one pass and after two that add
+    # up. Some sixteen roundings to 11 bits lie between the embedding and a gradient, each 2^-11 of its value at most:
+    # 0.8% of the norm, with logits' errors of up to |z| <= 3 times that in the softmax's share: 2%.
+    torch.manual_seed(11)
+    V, B, T = 20_000, 16, 128
+    model = lm.RecurrentLM(V, 16, layers=1, p=0.1, seed=4, dtype=torch.float16).to(DEV)
+    gen = torch.Generator(device=DEV).manual_seed(12)
+    tokens = torch.randint(V, (B, T + 1), generator=gen, device=DEV)
+    loss, want = reference_gradients(model, tokens[:, :-1], tokens[:, 1:], 0, 0)
+    for passes in (1, 2):
+        mean = model.loss_backward(tokens[:, :-1], tokens[:, 1:])
+        assert abs(float(mean) - float(loss)) <= 2.0 ** -9 * float(loss)
+        for n, p in model.named_parameters():
+            off = (p.grad.cpu().double() / passes - want[n]).norm() / want[n].norm()
+            assert off <= 0.02, (passes, n, float(off))
+    never = torch.ones(V, dtype=torch.bool, device=DEV)
+    never[tokens[:, 1:].flatten()] = False
+    assert (model.outer.bias.grad[never] > 0).all()
+
+
+def test_a_half_precision_model_when_most_targets_are_ignored():
+    # one target of 4,096 counts: the factor that holds the gradients up must not carry them over fp16's largest number
+    torch.manual_seed(13)
+    model = lm.RecurrentLM(500, 32, layers=2, p=0.0, dtype=torch.float16).to(DEV)
+    gen = torch.Generator(device=DEV).manual_seed(14)
+    tokens = torch.randint(500, (32, 129), generator=gen, device=DEV)
+    targets = torch.full((32, 128), -100, dtype=torch.int64, device=DEV)
+    targets[3, 100] = tokens[3, 101]
+    model.loss_backward(tokens[:, :-1], targets)
+    plain = lm.RecurrentLM(500, 32, layers=2, p=0.0).to(DEV)
+    plain.load_state_dict(model.state_dict())
+    plain.loss_backward(tokens[:, :-1], targets)
+    for (n, p), q in zip(model.named_parameters(), plain.parameters()):
+        assert torch.isfinite(p.grad).all(), n
+        assert (p.grad - q.grad).norm() <= 0.04 * q.grad.norm(), n  # two layers: twice the roundings of the test above
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16], ids=["f32", "f16"])
+def test_a_factor_of_the_logits_gradient_changes_no_other_gradient(dtype):
+    # gradients of the logits 64 times as large, the states' as they are: the same gradients of parameters and states. The
+    # factor is a power of two, so fp32 differs by orders of sums alone (200 terms of 2^-24), fp16 by its subnormals
+    torch.manual_seed(15)
+    model = lm.RecurrentLM(40, 32, layers=2, dtype=dtype).to(DEV).eval()
+    gen = torch.Generator(device=DEV).manual_seed(16)
+    tokens = torch.randint(40, (4, 9), generator=gen, device=DEV)
+    g = torch.randn((4, 9, 40), generator=gen, device=DEV).to(dtype)
+    gh = [torch.randn((4, 32), generator=gen, device=DEV) for _ in range(2)]
+    got = []
+    for factor in (1.0, 64.0):
+        state = [torch.ones((4, 32), device=DEV, requires_grad=True) for _ in range(2)]
+        logits, after = model(tokens, state, factor=factor)
+        model.zero_grad()
+        torch.autograd.backward([logits, *after], [g * factor, *gh])
+        got.append([p.grad for p in model.parameters()] + [s.grad for s in state])
+    for p, q in zip(*got):
+        assert (p - q).norm() <= (1e-5 if dtype == torch.float32 else 2.0 ** -8) * p.norm()
