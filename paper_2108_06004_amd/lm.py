@@ -13,9 +13,9 @@ Three operators, which one training step of such a model runs between its matrix
   over the logits, their gradient; ``cross_entropy`` under autograd.
 
 Tensors are fp32, bf16 or fp16 CUDA (ROCm) tensors of the current device (states, losses and
-statistics fp32); calls run on torch's current stream and do not wait. ``RecurrentLM`` is a language
-model of these operators; with ``train.GlobalSketchOptimizer`` its P workers' gradients go through the
-compression step.
+statistics fp32); calls run on torch's current stream and do not wait. An output that the caller gives
+counts for autograd as changed in place. ``RecurrentLM`` is a language model of these operators; with
+``train.GlobalSketchOptimizer`` its P workers' gradients go through the compression step.
 """
 from __future__ import annotations
 
@@ -89,6 +89,14 @@ def _written(t, name: str) -> None:
             raise ValueError(f"{name} must not be an expanded tensor")
 
 
+def _wrote(*given) -> None:
+    """Count the given outputs as changed in place, as torch's own operations do: a backward pass that needs what a
+    tensor held before is then an error."""
+    for t in given:
+        if t is not None:
+            torch.autograd.graph.increment_version(t)
+
+
 def _side(t, dtype, shape, device: int, name: str):
     """The pointer of a contiguous tensor of the given type and shape on `device` (None: NULL)."""
     if t is None:
@@ -122,6 +130,7 @@ def recurrence_forward(x, f, o=None, h0=None, lengths=None, save: bool = False, 
     itself for a step in place) are made unless given. save: also the states that ``recurrence_backward`` needs."""
     r, device, work = _recurrence(x, f, o, h0, lengths)
     B, T, C = x.shape
+    given = (y, h_last)
     y, to = _made(y, x, device, "y")
     if h_last is None:
         h_last = x.new_empty((B, C), dtype=torch.float32)
@@ -135,6 +144,7 @@ def recurrence_forward(x, f, o=None, h0=None, lengths=None, save: bool = False, 
                                                 saved.data_ptr() if save else None,
                                                 work.data_ptr() if work is not None else None),
            None, "gs_recurrence_forward")
+    _wrote(*given)
     return y, h_last, saved
 
 
@@ -147,6 +157,7 @@ def recurrence_backward(gy, x, f, o, saved, lengths=None, gh=None, dx=None, df=N
 
     if o is None and do is not None:
         raise ValueError("do is given but o is not")
+    given = (dx, df, do)
     dx, to_x = _made(dx, x, device, "dx")
     df, to_f = _made(df, x, device, "df")
     do, to_o = _made(do, x, device, "do") if o is not None else (None, gs_rows(None, 0, 0))
@@ -158,6 +169,7 @@ def recurrence_backward(gy, x, f, o, saved, lengths=None, gh=None, dx=None, df=N
                                                  to_f, to_o, dh0.data_ptr(),
                                                  work.data_ptr() if work is not None else None),
            None, "gs_recurrence_backward")
+    _wrote(*given)
     return dx, df, do, dh0
 
 
@@ -229,6 +241,7 @@ def _dropout(x, p, seed, site, step, residual, y):
     code, device = _activation(x, "x")
     if residual is not None:
         _like(residual, x, "residual")
+    given = y
     if y is None:
         y = torch.empty_like(x, memory_format=torch.contiguous_format)
     else:
@@ -246,6 +259,7 @@ def _dropout(x, p, seed, site, step, residual, y):
                                      residual.data_ptr() if residual is not None else None, rs, y.data_ptr(), ys, p,
                                      seed & U64, site & U64, _side(step, torch.int64, (1,), device, "step")),
            None, "gs_dropout")
+    _wrote(given)
     return y
 
 
@@ -316,11 +330,15 @@ def cross_entropy_forward(logits, targets, ignore_index: int = -100, grad=False,
     included: the gradient of factor * mean (the factor scales a loss of 16-bit gradients)."""
     out = logits.new_empty(logits.shape[:1], dtype=torch.float32)
     mean = logits.new_empty((), dtype=torch.float32)
+    given = None
     if grad is True:
         grad = torch.empty_like(logits, memory_format=torch.contiguous_format)
     elif grad is False:
         grad = None
+    else:
+        given = grad
     _cross_entropy(logits, targets, ignore_index, out, mean, grad, factor=factor, mean=True)
+    _wrote(given)
     return mean, out, grad
 
 

@@ -634,3 +634,42 @@ def test_refusals():
         lm.cross_entropy_forward(z[:, :0], t)
     with pytest.raises(gs.GsError):  # rows on top of each other
         lm.cross_entropy_forward(z.as_strided((3, 9), (4, 1)), t[:3])
+
+
+def test_a_written_tensor_counts_as_changed():
+    # torch's own rule for its in-place operations: a backward pass that needs what was there before is an error
+    i = inputs(51, 2, 12, 8, torch.float32)
+    z, t = logits(51, 6, 20, torch.float32)
+
+    def versions(**given):
+        return {k: v._version for k, v in given.items()}
+
+    def wrote(call, inputs_, **outs):
+        was, kept = versions(**outs), versions(**inputs_)
+        call(**outs)
+        assert all(outs[k]._version > was[k] for k in outs), call
+        assert versions(**inputs_) == kept
+
+    new = lambda: torch.empty_like(i["x"])  # noqa: E731
+    fixed = {k: i[k] for k in ("x", "f", "o", "gy", "gh")}
+    wrote(lambda **k: lm.recurrence_forward(i["x"], i["f"], i["o"], h0=i["h0"], **k), fixed, y=new(), h_last=i["h0"].clone())
+    wrote(lambda **k: lm.recurrence_forward(i["x"], i["f"], i["o"], h0=k["h_last"], **k), fixed, h_last=i["h0"].clone())
+    _, _, saved = lm.recurrence_forward(i["x"], i["f"], i["o"], h0=i["h0"], save=True)
+    wrote(lambda **k: lm.recurrence_backward(i["gy"], i["x"], i["f"], i["o"], saved, gh=i["gh"], **k),
+          {**fixed, "saved": saved}, dx=new(), df=new(), do=new())
+    wrote(lambda **k: lm.dropout_forward(i["x"], 0.5, 1, **k), fixed, y=new())
+    wrote(lambda **k: lm.dropout_backward(i["gy"], 0.5, 1, **k), fixed, dx=new())
+    wrote(lambda **k: lm.cross_entropy_forward(z, t, **k), dict(z=z, t=t), grad=torch.empty_like(z))
+    # tensors that an earlier node saved
+    for write in (lambda u: lm.dropout_forward(u, 0.5, 1, y=u),
+                  lambda u: lm.recurrence_forward(i["x"], i["f"], i["o"], y=u),
+                  lambda u: lm.cross_entropy_forward(u.view(-1, 8), torch.zeros(24, dtype=torch.int64, device=DEV),
+                                                     grad=u.view(-1, 8))):
+        u = i["x"].clone().requires_grad_() * 2
+        y, _ = lm.gated_recurrence(u, i["f"], i["o"], i["h0"])
+        write(u.detach())
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.sum().backward()
+    with torch.inference_mode():  # tensors without a version
+        u = i["x"].clone()
+        assert torch.equal(lm.dropout_forward(u, 0.5, 1, y=u), lm.dropout_forward(i["x"], 0.5, 1))
