@@ -23,8 +23,8 @@ import ctypes
 
 import torch
 
-from . import (GS_BF16, GS_F16, GS_F32, GS_RECURRENCE_BLOCK, GS_RECURRENCE_WHOLE, _check, gs_recurrence, gs_rows, gs_xent,
-               load_library)
+from . import (GS_BF16, GS_F16, GS_F32, GS_RECURRENCE_BLOCK, GS_RECURRENCE_MAX_STRIDE, GS_RECURRENCE_WHOLE, _check,
+               gs_recurrence, gs_rows, gs_xent, load_library)
 
 DTYPES = {torch.float32: GS_F32, torch.bfloat16: GS_BF16, torch.float16: GS_F16}
 U64 = (1 << 64) - 1
@@ -173,6 +173,13 @@ def recurrence_backward(gy, x, f, o, saved, lengths=None, gh=None, dx=None, df=N
     return dx, df, do, dh0
 
 
+def _taken(gy):
+    """A gradient as autograd hands it over, in a layout that the recurrence takes."""
+    _, T, C = gy.shape
+    _, st, sc = gy.stride()
+    return gy if (sc == 1 or C == 1) and (st <= GS_RECURRENCE_MAX_STRIDE or T == 1) else gy.contiguous()
+
+
 class _Recurrence(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, f, o, h0, lengths):
@@ -186,7 +193,7 @@ class _Recurrence(torch.autograd.Function):
     def backward(ctx, gy, gh):
         x, f, o, lengths, saved = ctx.saved_tensors
         gy = torch.zeros_like(x) if gy is None else gy
-        gy = gy if gy.stride(2) == 1 or gy.shape[2] == 1 else gy.contiguous()
+        gy = _taken(gy)
         gh = gh.contiguous() if gh is not None else None
         dx, df, do, dh0 = recurrence_backward(gy, x, f, o, saved, lengths, gh)
         return dx, df, do, dh0 if ctx.needs_input_grad[3] else None, None
@@ -209,7 +216,7 @@ class _PackedRecurrence(torch.autograd.Function):
         xfo, lengths, saved = ctx.saved_tensors
         parts = xfo.split(ctx.channels, -1)
         gy = torch.zeros(parts[0].shape, dtype=xfo.dtype, device=xfo.device) if gy is None else gy
-        gy = gy if gy.stride(2) == 1 or gy.shape[2] == 1 else gy.contiguous()
+        gy = _taken(gy)
         gh = gh.contiguous() if gh is not None else None
         grad = torch.empty(xfo.shape, dtype=xfo.dtype, device=xfo.device)
         to = grad.split(ctx.channels, -1)

@@ -673,3 +673,20 @@ def test_a_written_tensor_counts_as_changed():
     with torch.inference_mode():  # tensors without a version
         u = i["x"].clone()
         assert torch.equal(lm.dropout_forward(u, 0.5, 1, y=u), lm.dropout_forward(i["x"], 0.5, 1))
+
+
+def test_a_gradient_of_any_time_stride_goes_backward():
+    # autograd hands over whatever layout the gradient has; here one that the kernels do not take
+    wide = gs.GS_RECURRENCE_MAX_STRIDE + 8
+    for C in (1, 8):
+        i = inputs(52, 2, 2, C, torch.bfloat16)
+        gy = torch.empty(3 * wide, dtype=torch.bfloat16, device=DEV).as_strided((2, 2, C), (wide // 2, wide, 1))
+        gy.copy_(i["gy"])
+        want = ref.recurrence(i["x"], i["f"], i["o"], i["h0"], None, i["gy"], None)
+        leaf = i["x"].clone().requires_grad_()
+        lm.gated_recurrence(leaf, i["f"], i["o"], i["h0"])[0].backward(gy)
+        ref.check(leaf.grad, want["dx"], torch.bfloat16, "dx")
+        leaf = torch.cat([i["x"], i["f"], i["o"]], -1).requires_grad_()
+        lm.gated_recurrence_packed(leaf, C, i["h0"])[0].backward(gy)
+        for n, k in enumerate(("dx", "df", "do")):
+            ref.check(leaf.grad[:, :, n * C:(n + 1) * C], want[k], torch.bfloat16, k)
