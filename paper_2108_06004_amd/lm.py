@@ -199,10 +199,15 @@ class _Recurrence(torch.autograd.Function):
         return dx, df, do, dh0 if ctx.needs_input_grad[3] else None, None
 
 
+def _parts(xfo, channels: int):
+    """x, f and o (or x and f) of a projection; three of no channels where it has none."""
+    return xfo.split(channels, -1) if channels else (xfo, xfo, xfo)
+
+
 class _PackedRecurrence(torch.autograd.Function):
     @staticmethod
     def forward(ctx, xfo, channels, h0, lengths):
-        parts = xfo.split(channels, -1)
+        parts = _parts(xfo, channels)
         y, h_last, saved = recurrence_forward(parts[0], parts[1], parts[2] if len(parts) == 3 else None, h0, lengths,
                                               save=any(ctx.needs_input_grad))
         ctx.save_for_backward(xfo, lengths, saved)
@@ -214,12 +219,12 @@ class _PackedRecurrence(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, gy, gh):
         xfo, lengths, saved = ctx.saved_tensors
-        parts = xfo.split(ctx.channels, -1)
+        parts = _parts(xfo, ctx.channels)
         gy = torch.zeros(parts[0].shape, dtype=xfo.dtype, device=xfo.device) if gy is None else gy
         gy = _taken(gy)
         gh = gh.contiguous() if gh is not None else None
         grad = torch.empty(xfo.shape, dtype=xfo.dtype, device=xfo.device)
-        to = grad.split(ctx.channels, -1)
+        to = _parts(grad, ctx.channels)
         gate = len(parts) == 3
         _, _, _, dh0 = recurrence_backward(gy, parts[0], parts[1], parts[2] if gate else None, saved, lengths, gh,
                                            dx=to[0], df=to[1], do=to[2] if gate else None)

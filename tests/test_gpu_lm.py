@@ -690,3 +690,12 @@ def test_a_gradient_of_any_time_stride_goes_backward():
         lm.gated_recurrence_packed(leaf, C, i["h0"])[0].backward(gy)
         for n, k in enumerate(("dx", "df", "do")):
             ref.check(leaf.grad[:, :, n * C:(n + 1) * C], want[k], torch.bfloat16, k)
+
+
+def test_a_packed_recurrence_without_channels():
+    for T in (0, 5):
+        xfo = torch.empty((3, T, 0), device=DEV, requires_grad=True)
+        y, h = lm.gated_recurrence_packed(xfo, 0)
+        assert y.shape == (3, T, 0) and h.shape == (3, 0)
+        y.sum().backward()
+        assert xfo.grad.shape == xfo.shape
