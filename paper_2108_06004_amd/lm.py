@@ -473,9 +473,11 @@ class RecurrentLM(torch.nn.Module):
         """The `count` likeliest next tokens, one at a time, after tokens ([B][T], T >= 1): int64 [B][count]."""
         was, out = self.training, []
         self.eval()
-        logits, state = self(tokens)
-        for _ in range(count):
-            out.append(logits[:, -1].argmax(-1))
-            logits, state = self(out[-1][:, None], state)
-        self.train(was)
+        try:
+            logits, state = self(tokens)
+            for _ in range(count):
+                out.append(logits[:, -1].argmax(-1))
+                logits, state = self(out[-1][:, None], state)
+        finally:
+            self.train(was)
         return torch.stack(out, 1) if out else tokens[:, :0]

@@ -152,3 +152,13 @@ def test_operators_refuse_tensors_off_the_gpu():
         lm.cross_entropy(x[0], torch.zeros(3, dtype=torch.int64), reduction="sum")
     with pytest.raises(TypeError):
         lm.RecurrentLM(10, 4, dtype=torch.float64)
+
+
+def test_a_failed_generation_leaves_the_training_mode():
+    torch = pytest.importorskip("torch")
+    from paper_2108_06004_amd import lm
+
+    model = lm.RecurrentLM(10, 4)
+    with pytest.raises(TypeError):  # not on the GPU
+        model.generate(torch.zeros((1, 2), dtype=torch.int64), 1)
+    assert model.training
