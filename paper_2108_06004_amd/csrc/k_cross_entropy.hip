@@ -51,11 +51,12 @@ __device__ __forceinline__ Seen join(Seen p, Seen q) {
 // The sum of the losses and the rows that count.
 struct Tally {
   double sum;
-  float n;
+  int n;
 };
 
 // A value of the lane whose number differs in bit d.
 __device__ __forceinline__ float lane_xor(float v, int d) { return __shfl_xor(v, d); }
+__device__ __forceinline__ int lane_xor(int v, int d) { return __shfl_xor(v, d); }
 __device__ __forceinline__ Seen lane_xor(Seen s, int d) { return Seen{__shfl_xor(s.top, d), __shfl_xor(s.sum, d)}; }
 __device__ __forceinline__ Tally lane_xor(Tally t, int d) { return Tally{__shfl_xor(t.sum, d), __shfl_xor(t.n, d)}; }
 
@@ -72,8 +73,9 @@ __device__ __forceinline__ T block_reduce(T v, T* lds, F f) {
   return v;
 }
 
-// The rows that count among those of one lane, eight loads at a time.
-__device__ __forceinline__ float count_of(const gs_xent& x, int lane, int lanes) {
+// The rows that count among those of one lane, eight loads at a time. Counts are whole numbers up to 2^31 - 1 and are rounded
+// to fp32 once, as a divisor.
+__device__ __forceinline__ int count_of(const gs_xent& x, int lane, int lanes) {
   int n = 0;
   for (int64_t i0 = lane; i0 < x.N; i0 += 8 * lanes) {
     int64_t t[8];
@@ -82,21 +84,22 @@ __device__ __forceinline__ float count_of(const gs_xent& x, int lane, int lanes)
 #pragma unroll
     for (int u = 0; u < 8; ++u) n += t[u] != x.ignore_index;
   }
-  return (float)n;
+  return n;
 }
 
-// counts below 2^24 a thread are whole numbers in fp32; their sum is rounded as a whole
+__device__ __forceinline__ float inverse_of(int n) { return 1.0f / (float)(n > 1 ? n : 1); }
+
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS) k_xent_count(gs_xent x) {
-  __shared__ float lds[THREADS / 64];
-  const float n = block_reduce<THREADS>(count_of(x, threadIdx.x, THREADS), lds, [](float p, float q) { return p + q; });
-  if (threadIdx.x == 0) *static_cast<float*>(x.work) = 1.0f / fmaxf(n, 1.0f);
+  __shared__ int lds[THREADS / 64];
+  const int n = block_reduce<THREADS>(count_of(x, threadIdx.x, THREADS), lds, [](int p, int q) { return p + q; });
+  if (threadIdx.x == 0) *static_cast<float*>(x.work) = inverse_of(n);
 }
 
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS) k_xent_mean(gs_xent x) {
   __shared__ Tally lds[THREADS / 64];
-  Tally t{0.0, 0.0f};
+  Tally t{0.0, 0};
   for (int64_t i0 = threadIdx.x; i0 < x.N; i0 += 8 * THREADS) {
     float loss[8];
 #pragma unroll
@@ -106,19 +109,19 @@ __global__ void __launch_bounds__(THREADS) k_xent_mean(gs_xent x) {
   }
   t.n = count_of(x, threadIdx.x, THREADS);
   t = block_reduce<THREADS>(t, lds, [](Tally p, Tally q) { return Tally{p.sum + q.sum, p.n + q.n}; });
-  if (threadIdx.x == 0) *x.mean_loss = (float)(t.sum / fmaxf(t.n, 1.0f));
+  if (threadIdx.x == 0) *x.mean_loss = (float)(t.sum / (t.n > 1 ? t.n : 1));
 }
 
-// The factor of a row's gradient. Rows few enough are counted here, by the first wave's lanes.
+// The factor of a row's gradient. Rows few enough are counted here, by each wave on its own.
 __device__ __forceinline__ float factor_of(const gs_xent& x, int64_t n) {
   float m = x.factor;
   if (x.scale) m *= x.scale[n * x.scale_stride];
   if (x.mean) {
     if (x.N <= kInlineCount) {
-      float c = count_of(x, threadIdx.x & 63, 64);
+      int c = count_of(x, threadIdx.x & 63, 64);
 #pragma unroll
       for (int d = 32; d > 0; d >>= 1) c += __shfl_xor(c, d);
-      m *= 1.0f / fmaxf(c, 1.0f);
+      m *= inverse_of(c);
     } else {
       m *= *static_cast<const float*>(x.work);
     }

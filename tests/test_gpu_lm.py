@@ -699,3 +699,16 @@ def test_a_packed_recurrence_without_channels():
         assert y.shape == (3, T, 0) and h.shape == (3, 0)
         y.sum().backward()
         assert xfo.grad.shape == xfo.shape
+
+
+def test_cross_entropy_counts_rows_past_the_whole_numbers_of_fp32():
+    # 2^25 + 16 rows that count, each of loss log 2: their mean is log 2, each rounding of the loss, the count and the quotient
+    # within 2^-24 of it, log 2's own evaluation within 2^-23
+    N = (1 << 25) + 1024
+    z = torch.zeros((N, 2), dtype=torch.bfloat16, device=DEV)
+    t = torch.zeros(N, dtype=torch.int64, device=DEV)
+    last = t[N - 1024:]
+    last[torch.arange(1024, device=DEV) % 64 != 0] = -100
+    mean, losses, _ = lm.cross_entropy_forward(z, t)
+    assert (losses[:N - 1024] == losses[0]).all() and abs(float(losses[0]) - 0.6931471805599453) <= 2.0 ** -23
+    assert abs(float(mean) / float(losses[0]) - 1) <= 2.0 ** -23
