@@ -103,9 +103,8 @@ struct Block {
 template <int DT, int VEC, int AUX>
 __device__ __forceinline__ typename Pack<DT, VEC>::raw load(const Block& k, uint32_t off, uint32_t step) {
   using raw = typename Pack<DT, VEC>::raw;
-  if constexpr (sizeof(raw) == 8)
-    return __builtin_bit_cast(raw, __builtin_amdgcn_raw_buffer_load_b64(k.at, off, step * k.time, AUX));
-  else if constexpr (sizeof(raw) == 4)
+  static_assert(sizeof(raw) == 4 || sizeof(raw) == 2, "one channel a lane, or two of 16 bits");
+  if constexpr (sizeof(raw) == 4)
     return __builtin_bit_cast(raw, __builtin_amdgcn_raw_buffer_load_b32(k.at, off, step * k.time, AUX));
   else
     return __builtin_bit_cast(raw, __builtin_amdgcn_raw_buffer_load_b16(k.at, off, step * k.time, AUX));
@@ -114,10 +113,7 @@ __device__ __forceinline__ typename Pack<DT, VEC>::raw load(const Block& k, uint
 template <int DT, int VEC, int AUX>
 __device__ __forceinline__ void store(const Block& k, uint32_t off, uint32_t step, typename Pack<DT, VEC>::wide v) {
   const auto raw = Pack<DT, VEC>::down(v);
-  if constexpr (sizeof raw == 8) {
-    typedef uint32_t u2 __attribute__((ext_vector_type(2)));
-    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u2, raw), k.at, off, step * k.time, AUX);
-  } else if constexpr (sizeof raw == 4) {
+  if constexpr (sizeof raw == 4) {
     __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, raw), k.at, off, step * k.time, AUX);
   } else {
     __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, raw), k.at, off, step * k.time, AUX);
