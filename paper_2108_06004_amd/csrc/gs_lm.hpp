@@ -40,9 +40,10 @@ struct Pack {
 
 constexpr float kLog2e = 1.44269504088896340736f;
 
-// sigmoid(z) and 1 - sigmoid(z) = sigmoid(-z), each to a few ulp of itself (1 - s would lose the
-// digits of a gate near one): with e = exp(-z) they are 1 / (1 + e) and e / (1 + e). Where e is so large that
-// the first is 0 or no normal number the second is 1 (e may be infinite there); a NaN stays one.
+// sigmoid(z) and 1 - sigmoid(z) = sigmoid(-z), each to its own digits (1 - s would lose those of a gate near one): with
+// e = exp(-z) they are 1 / (1 + e) and e / (1 + e). Each is off by at most (1.25 |z| + 8) 2^-24 of itself, the first part
+// from z log2(e), which is rounded once: what half an ulp of an fp32 z changes. Where e is so large that the
+// first is 0 or no normal number the second is 1 (e may be infinite there); a NaN stays one.
 __device__ __forceinline__ void sigmoid_both(float z, float& s, float& rest) {
   const float e = __builtin_amdgcn_exp2f(-z * kLog2e);
   s = __builtin_amdgcn_rcpf(1.0f + e);

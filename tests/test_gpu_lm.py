@@ -712,3 +712,17 @@ def test_cross_entropy_counts_rows_past_the_whole_numbers_of_fp32():
     mean, losses, _ = lm.cross_entropy_forward(z, t)
     assert (losses[:N - 1024] == losses[0]).all() and abs(float(losses[0]) - 0.6931471805599453) <= 2.0 ** -23
     assert abs(float(mean) / float(losses[0]) - 1) <= 2.0 ** -23
+
+
+def test_recurrence_gates_over_the_range_of_fp32():
+    # from h = 0 and x = 1 one step gives 1 - a, from h = 1 and x = 0 it gives a. The exponential's argument z log2(e) is off
+    # by 1.23 u of itself (the constant's rounding and the product's), which is 1.23 |z| u of the result; the exponential, the
+    # sum, the reciprocal and a product add at most 8 u. Below 2^-125 a gate may be 0.
+    z = torch.linspace(-95, 95, 20_001).view(1, 1, -1).to(DEV)
+    one, none = torch.ones_like(z), torch.zeros_like(z)
+    f = z.double().cpu()
+    for x, h0, want in ((one, none, 1 / (1 + torch.exp(f))), (none, one, 1 / (1 + torch.exp(-f)))):
+        y, h, _ = lm.recurrence_forward(x, z, h0=h0[0].contiguous())
+        assert torch.equal(y[0], h)
+        off = (y.double().cpu() - want).abs() - 2.0 ** -125
+        assert (off <= (1.25 * f.abs() + 8) * 2.0 ** -24 * want).all()
