@@ -6,7 +6,7 @@
 // several workgroups: one kernel reduces each part to (maximum, sum), a second joins them and writes the
 // gradient, reading the logits again.
 //
-// What bounds it: memory (4,096 x 22,000 bf16 with gradient: 70 us, 5.1 TB/s; 8,191 x 131,071: 852 us, 5.0 TB/s, one
+// What bounds it: memory (4,096 x 22,000 bf16 with gradient: 65 us, 5.4 TB/s; 8,191 x 131,071: 852 us, 5.0 TB/s, one
 // workgroup a CU), and for few rows the launches: the row's kernel 4.7 us and the mean's 1.8 at 35 x 22,000 fp32.
 //
 // Rows need not be aligned: the elements before the first 16-byte boundary of a row and after its last one
@@ -17,8 +17,8 @@ namespace gs {
 namespace {
 
 constexpr int kTail = 1024;  // threads that count rows and sum losses
-// So many rows every workgroup counts by itself; more are counted by a kernel before (with 4,096 rows of 22,000
-// logits counting in the row's kernel took 80 us against 69 and the kernel's 5: the targets' loads displace the row's).
+// So many rows every wave counts by itself; more are counted by a kernel before (4,096 rows of 22,000 bf16 logits,
+// whole call: 128 us counted in the row's kernel, whose own loads the targets' displace, 72 before it; 300 rows: 14.1 and 16.4).
 constexpr int kInlineCount = 256;
 constexpr int kPartThreads = 256;
 constexpr int kPartVecs = 4;          // 16-byte pieces a thread takes of a part, at least
@@ -157,8 +157,8 @@ struct Row {
   __device__ __forceinline__ int edge(int i) const {
     return i < head ? i : i < head + tail ? head + vecs * N + (i - head) : -1;
   }
-  // Pieces read for the last time and gradients go past the caches (PAST; 4,096 x 22,000 bf16 with gradient: 81 us
-  // through them, 78 past; 2,000 x 32,000 fp32 106 and 98), but for the longest rows where they do not fill their
+  // Pieces read for the last time and gradients go past the caches (PAST; 4,096 x 22,000 bf16 with gradient: 78 us
+  // through them, 72 past; 2,000 x 32,000 fp32 106 and 98), but for the longest rows where they do not fill their
   // 128-byte lines (8,191 x 131,071 bf16: 873 us through the caches, 902 past).
   template <bool PAST>
   __device__ __forceinline__ typename P::raw get(int j) const {
@@ -403,6 +403,9 @@ template <int DT, bool GRAD, bool SAME>
 void rows(hipStream_t s, const gs_xent& x) {
   const int64_t vecs = x.V / (16 / elem_size(DT));
   const dim3 grid = grid_of(x.N);
+  // The fewest threads whose pieces hold the row, one to four pieces a thread in a wave, two to eight from 256 threads on.
+  // 2,049 to 3,072 pieces go to 512 threads as well as more do: twelve a thread of 256 took longer (4,096 rows with gradient:
+  // 20,000 bf16 logits 70 us for 66, 22,000 78 for 72.5, 24,500 86 for 80; 11,000 fp32 74 for 71; 2,000 x 8,400 33.6 for 31.5).
 #define GS_XENT(THREADS, CH) \
   if (vecs <= (THREADS) * (CH)) return k_xent_row<DT, THREADS, CH, GRAD, SAME><<<grid, THREADS, 0, s>>>(x), void()
   GS_XENT(64, 1);
@@ -411,7 +414,6 @@ void rows(hipStream_t s, const gs_xent& x) {
   GS_XENT(256, 2);
   GS_XENT(256, 4);
   GS_XENT(256, 8);
-  GS_XENT(256, 12);
   GS_XENT(512, 8);
   GS_XENT(1024, 8);
 #undef GS_XENT

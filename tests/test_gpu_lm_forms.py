@@ -29,7 +29,7 @@ def test_recurrence_of_many_sequences(B, T, C, dtype):
     run_and_check(whole, what="whole")
 
 
-# (3,072, 4,096] pieces of 16 bytes: 512 threads; (8,192, 16,384] and more rows than are split: 1,024 threads of sixteen
+# (2,048, 4,096] pieces of 16 bytes: 512 threads; (8,192, 16,384] and more rows than are split: 1,024 threads of sixteen
 # pieces, through the caches or, rows of whole 128-byte lines, past them; more pieces: split, first read past the caches
 # from 65 rows on; from 257 rows on the divisor shares the scratch with the parts
 @pytest.mark.parametrize("N,V", [(5, 30_000), (65, 70_001), (65, 70_016), (65, 131_201)])
