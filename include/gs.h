@@ -369,6 +369,7 @@ gs_status gs_recurrence_forward(const gs_recurrence* r, void* stream, gs_rows y,
  *     dx_t = (1 - a_t) s_t,   df_t = s_t (h_(t-1) - x_t) a_t (1 - a_t),
  *     do_t = gy_t h_t sigmoid(o_t) (1 - sigmoid(o_t)),   dh0 = a_1 s_1;   zero at padding.
  * The states h_t are computed again from `states` of the forward call on the same inputs.
+ * Time is joined as in the forward call: an infinite gradient of a state may become NaN.
  * gy: [B][T][C] input. gh: [B][C] fp32 input, the gradient of h_last, or NULL (zero). dx, df, dout:
  * [B][T][C] outputs (dout.data NULL exactly when there is no o). dh0: [B][C] fp32 output or NULL.
  * Outputs must not overlap inputs. */

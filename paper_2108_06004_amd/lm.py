@@ -127,7 +127,8 @@ def recurrence_forward(x, f, o=None, h0=None, lengths=None, save: bool = False, 
     x, f, o: candidates, forget-gate and output-gate pre-activations, channels contiguous (o may be
     None: y is the state). h0: [B][C] fp32 or None (zero). lengths: int32 [B] or None; positions from
     a sequence's length on are padding: they keep its state and give y = 0. y and h_last ([B][C] fp32, h0
-    itself for a step in place) are made unless given. save: also the states that ``recurrence_backward`` needs."""
+    itself for a step in place) are made unless given and overlap no other input. Strides are free, but with T > 1 a time
+    stride is at most GS_RECURRENCE_MAX_STRIDE elements. save: also the states that ``recurrence_backward`` needs."""
     r, device, work = _recurrence(x, f, o, h0, lengths)
     B, T, C = x.shape
     given = (y, h_last)
@@ -151,7 +152,7 @@ def recurrence_forward(x, f, o=None, h0=None, lengths=None, save: bool = False, 
 def recurrence_backward(gy, x, f, o, saved, lengths=None, gh=None, dx=None, df=None, do=None):
     """The gradients ``(dx, df, do, dh0)`` of the recurrence. gy: [B][T][C], the gradient of y; gh:
     [B][C] fp32, that of h_last, or None; saved: the forward call's, on the same inputs. dx, df and do are
-    made unless given (do is None without o)."""
+    made unless given (do is None without o) and overlap no input."""
     r, device, work = _recurrence(x, f, o, None, lengths)
     B, T, C = x.shape
 
@@ -337,7 +338,7 @@ def _cross_entropy(logits, targets, ignore_index, losses, mean_loss, grad, facto
 
 def cross_entropy_forward(logits, targets, ignore_index: int = -100, grad=False, factor: float = 1.0):
     """``(mean, losses, dlogits)`` of softmax cross-entropy in one pass over the logits. logits: [N][V], rows
-    contiguous; targets: int64 [N]. mean: fp32 scalar, over the rows whose target is not ignore_index (0 when there is
+    contiguous; targets: int64 [N], contiguous. mean: fp32 scalar, over the rows whose target is not ignore_index (0 when there is
     none); losses: fp32 [N]. grad: False (dlogits is None), True, or a tensor to write, the logits themselves
     included: the gradient of factor * mean (the factor scales a loss of 16-bit gradients)."""
     out = logits.new_empty(logits.shape[:1], dtype=torch.float32)
